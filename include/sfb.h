@@ -295,6 +295,65 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
                          float *U, int64_t ldu, void *V, int64_t ldv, float *loss, float eta,
                          const uint8_t *active, sfb_prox_kind kind, float param);
 
+/*
+ * AdamW over many tensors at once, an alternative to W <- W - eta dW with moments of the gradient.  With g' = grad_scale * g,
+ * t the step being taken (the first is 1):
+ *     m <- beta1 m + (1 - beta1) g'         v <- beta2 v + (1 - beta2) g'^2
+ *     p <- p - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)
+ * Any context serves: only its stream (and its GPU) is used.
+ *   step        DEVICE [1] int32, the steps taken so far (0 before the first); the call adds 1, so a captured call goes on counting
+ *   grad_scale  DEVICE [1] fp32 or NULL (1): the factor that sfb_grad_norm leaves.  NaN: the call changes nothing, step included
+ *   lr_scale    DEVICE [1] fp32 or NULL (1): multiplies lr, for a rate that changes under a captured call
+ *   state_bits  32: m, v fp32.  8: one byte an element each, with a scale for every 128 elements of a tensor, a power of two
+ *               whose exponent + 127 stands in m_scale, v_scale [(n + 127) / 128].  m: sign, 4 exponent bits of bias 7, 3 mantissa bits.
+ *               v: 5 exponent bits of bias 15, 3 mantissa bits.  p moves by the moments before they are rounded, and they are
+ *               rounded up or down at random in proportion (1 - beta2 of v is far less than the distance of two codes), from `seed`, the
+ *               step and the element's number; the same call on the same state gives the same bits.  All bytes 0 is a state of zeros.
+ *               A moment above 0 of v keeps the smallest code; NaN and infinities become NaN and have no part in the scale.
+ * Tensors are dense, at any alignment of their type (16 bytes, and 8 for codes, take wide accesses); none may overlap another.
+ * n = 0 is skipped.  SFB_EINVAL: a null pointer that is needed, count < 0, a rate that is not finite or negative, a beta outside [0, 1), state_bits
+ * neither 32 nor 8; SFB_ESHAPE: n < 0 or beyond 2^40; SFB_EDTYPE.  Nothing is launched if an argument is refused.
+ * Timed under family 7.
+ */
+typedef struct sfb_adamw_tensor {
+    float *p;                    /* [n] in and out */
+    const void *g;               /* [n] in grad_dtype */
+    void *m;                     /* [n] */
+    void *v;                     /* [n] */
+    uint8_t *m_scale;            /* state_bits 8 only, else NULL */
+    uint8_t *v_scale;
+    void *copy;                  /* [n] bf16 out: p rounded, or NULL */
+    int64_t n;
+} sfb_adamw_tensor;
+typedef struct sfb_adamw {
+    float lr, beta1, beta2, eps, weight_decay;
+    int32_t state_bits;
+    sfb_dtype grad_dtype;
+    uint32_t seed;
+    int32_t *step;
+    const float *grad_scale;
+    const float *lr_scale;
+} sfb_adamw;
+SFB_API sfb_status sfb_adamw_step(sfb_ctx *ctx, const sfb_adamw_tensor *tensors, int32_t count, const sfb_adamw *opt);
+/* The values of 8-bit moments as bf16 (exact): tensor i's to m_out[i] and v_out[i], HOST arrays of DEVICE pointers [n].  Of `tensors`
+ * only m, v, their scales and n are read. */
+SFB_API sfb_status sfb_adamw_unpack(sfb_ctx *ctx, const sfb_adamw_tensor *tensors, int32_t count, void *const *m_out, void *const *v_out);
+/*
+ * The norm of many gradients taken as one vector, and the factor that clips them, both left on the device:
+ *     out[0] = norm = sqrt(sum g^2)      out[1] = min(1, max_norm / norm), NaN if the norm is not finite
+ * out: DEVICE [2] fp32.  The sum is taken in 64 bits in a fixed order.  ws: DEVICE, 8-byte aligned, at least sfb_grad_norm_bytes; it
+ * belongs to the call until that has run (calls that may overlap in time need one each).
+ * SFB_EINVAL: a null pointer, count < 0, max_norm not positive (infinity: no clipping); SFB_ESHAPE: n < 0 or beyond 2^40;
+ * SFB_EDTYPE; SFB_EWORKSPACE.
+ */
+typedef struct sfb_gradient {
+    const void *g;               /* [n] */
+    int64_t n;
+} sfb_gradient;
+SFB_API sfb_status sfb_grad_norm_bytes(const sfb_gradient *grads, int32_t count, size_t *bytes);
+SFB_API sfb_status sfb_grad_norm(sfb_ctx *ctx, const sfb_gradient *grads, int32_t count, sfb_dtype grad_dtype, float max_norm, float *out,
+                                 void *ws, size_t ws_bytes);
+
 /* What the context was created with; any pointer may be NULL. */
 SFB_API sfb_status sfb_shape(const sfb_ctx *ctx, int64_t *J, int64_t *D, int32_t *P, int32_t *B,
                      int32_t *input_dtype);
@@ -324,7 +383,8 @@ SFB_API int sfb_last_hip_error(const sfb_ctx *ctx);
  * (0 = scores, or the one-pass kernel of few classes, without the kernel that adds its planes; 1 = factor u, 2 =
  * reconstruct-apply: the contraction, without the kernels that pack bf16 operands, copy ragged factors, make the stored
  * entries' lists or add planes, 3 = CSR densify / stream copy, 4 = proximal step, 5 = the one-pass update +
- * next scores kernel of sfb_step_pipelined, without its packing kernel) since the last reset.
+ * next scores kernel of sfb_step_pipelined, without its packing kernel, 7 = AdamW and gradient norms, the first launch of
+ * a call) since the last reset.
  */
 SFB_API sfb_status sfb_plan_info(const sfb_ctx *ctx, int32_t *fwd_split_k, int32_t *fwd_grid,
                          int32_t *recon_grid);

@@ -32,6 +32,21 @@ class sfb_sdca(C.Structure):
                 ("conj", C.c_void_p), ("lam", C.c_float), ("s", C.c_float)]
 
 
+class sfb_adamw_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64)]
+
+
+class sfb_adamw(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float), ("weight_decay", C.c_float),
+                ("state_bits", C.c_int32), ("grad_dtype", C.c_int), ("seed", C.c_uint32), ("step", C.c_void_p),
+                ("grad_scale", C.c_void_p), ("lr_scale", C.c_void_p)]
+
+
+class sfb_gradient(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("n", C.c_int64)]
+
+
 def _load():
     path = library_path()
     if not os.path.exists(path):
@@ -75,6 +90,10 @@ def _load():
         "sfb_prox": (C.c_int, [vp, vp, i64, C.c_int, f32, f32]),
         "sfb_reconstruct_apply_prox": (C.c_int, [vp, vp, i64, vp, i64, vp, i64, f32, f32, vp, C.c_int, f32]),
         "sfb_step_prox": (C.c_int, [vp, vp, i64, pb, vp, vp, i64, vp, i64, vp, f32, vp, C.c_int, f32]),
+        "sfb_adamw_step": (C.c_int, [vp, C.POINTER(sfb_adamw_tensor), i32, C.POINTER(sfb_adamw)]),
+        "sfb_adamw_unpack": (C.c_int, [vp, C.POINTER(sfb_adamw_tensor), i32, C.POINTER(vp), C.POINTER(vp)]),
+        "sfb_grad_norm_bytes": (C.c_int, [C.POINTER(sfb_gradient), i32, C.POINTER(C.c_size_t)]),
+        "sfb_grad_norm": (C.c_int, [vp, C.POINTER(sfb_gradient), i32, C.c_int, f32, vp, vp, C.c_size_t]),
         "sfb_ssp_create": (C.c_int, [C.POINTER(vp), vp, i32, C.POINTER(vp), i64, vp, i64, vp, i64, i32]),
         "sfb_ssp_destroy": (None, [vp]),
         "sfb_ssp_worker_step": (C.c_int, [vp, i32, pb, vp, f32, vp, C.POINTER(i32)]),

@@ -15,7 +15,9 @@
 using namespace sfb;
 
 namespace {
-constexpr int kFamilies = 6;  // 0 scores, 1 factor u, 2 reconstruct-apply, 3 sparse helpers, 4 proximal step, 5 one-pass update + next scores
+constexpr int kFamilies = 9;  // 0 scores, 1 factor u, 2 reconstruct-apply, 3 sparse helpers, 4 proximal step, 5 one-pass update + next scores,
+                              // 7 AdamW and gradient norms, 8 cross entropy of a head (6 stands for nothing and is refused)
+constexpr bool is_family(int which) { return which >= 0 && which < kFamilies && which != 6; }
 struct EventPair { hipEvent_t a, b; };
 struct LastKernel { const char* name; uint32_t grid; };   // what SFB_LAUNCH left
 
@@ -61,6 +63,7 @@ struct sfb_ctx {
     int32_t P, B;
     sfb_dtype dtype;
     hipStream_t stream;
+    int device;                    // current when the context was created; -1: no GPU
     FwdPlan fwd_all, fwd_worker;   // scores of all N rows / of one worker's B rows
     FwdPlan fwd_bf16;              // all N rows on the bf16 matrix cores (bf16 contexts)
     Bf16TilePlan tile_scores[2][2];   // bf16 contexts: scores in tiles, all rows or one worker's, W rounded or exact
@@ -229,6 +232,19 @@ struct Timed {
         } else {
             c->used[fam].push_back(ev);
         }
+    }
+};
+
+// The context's GPU is current while a call launches, whichever was before and is afterwards.
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(const sfb_ctx* c) {
+        int now = -1;
+        if (c->device < 0 || hipGetDevice(&now) != hipSuccess || now == c->device) return;
+        if (hipSetDevice(c->device) == hipSuccess) before = now;
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
     }
 };
 
@@ -519,6 +535,10 @@ sfb_status sfb_create(sfb_ctx** out, sfb_model m, int64_t J, int64_t D, int32_t 
     if (!c) return SFB_EINVAL;
     c->model = m; c->J = J; c->D = D; c->P = P; c->B = B; c->dtype = input_dtype;
     c->stream = (hipStream_t)hip_stream;
+    if (hipGetDevice(&c->device) != hipSuccess) {
+        c->device = -1;
+        (void)hipGetLastError();
+    }
     c->fwd_all = plan_forward((int64_t)P * B, J, D);
     c->fwd_worker = plan_forward(B, J, D);
     c->fwd_bf16 = plan_forward_bf16((int64_t)P * B, J, D);
@@ -881,7 +901,7 @@ sfb_status sfb_plan_info(const sfb_ctx* c, int32_t* fwd_split_k, int32_t* fwd_gr
 }
 
 sfb_status sfb_last_kernel(const sfb_ctx* c, int32_t which, char* name, size_t bytes, int32_t* grid) {
-    if (!c || which < 0 || which >= kFamilies || (name && bytes == 0)) return SFB_EINVAL;
+    if (!c || !is_family(which) || (name && bytes == 0)) return SFB_EINVAL;
     if (name) {                                                  // as it stands at the launch, up to its template arguments
         const char* k = c->last[which].name ? c->last[which].name : "";
         if (*k == '(') ++k;
@@ -999,7 +1019,7 @@ sfb_status sfb_enable_timing(sfb_ctx* c, int enable) {
 }
 
 sfb_status sfb_kernel_time_ms(sfb_ctx* c, int which, double* ms, int64_t* launches) {
-    if (!c || which < 0 || which >= kFamilies || !ms) return SFB_EINVAL;
+    if (!c || !is_family(which) || !ms) return SFB_EINVAL;
     hipError_t e = hipStreamSynchronize(c->stream);
     if (e != hipSuccess) return hip_fail(c, e);
     double total = 0.0;
@@ -1022,6 +1042,111 @@ sfb_status sfb_reset_timing(sfb_ctx* c) {
         for (auto& p : c->used[f]) c->spare.push_back(p);
         c->used[f].clear();
     }
+    return SFB_OK;
+}
+
+// ---- AdamW over many tensors, the norm of many gradients ---------------------------------------------------------
+
+static constexpr int64_t kMostElements = 1LL << 40;
+static bool aligned(const void* p, size_t to) { return ((uintptr_t)p % to) == 0; }
+
+sfb_status sfb_adamw_step(sfb_ctx* c, const sfb_adamw_tensor* tensors, int32_t count, const sfb_adamw* o) {
+    if (!c || !o || count < 0 || (count > 0 && !tensors) || !o->step) return SFB_EINVAL;
+    if (o->grad_dtype != SFB_F32 && o->grad_dtype != SFB_BF16) return SFB_EDTYPE;
+    if (o->state_bits != 32 && o->state_bits != 8) return SFB_EINVAL;
+    for (const float x : {o->lr, o->eps, o->weight_decay})
+        if (!std::isfinite(x) || x < 0.f) return SFB_EINVAL;
+    for (const float b : {o->beta1, o->beta2})
+        if (!(b >= 0.f && b < 1.f)) return SFB_EINVAL;
+    std::vector<AdamwTensor> list;
+    try {
+        list.resize((size_t)count);
+    } catch (...) {
+        return SFB_EINVAL;
+    }
+    const bool bits8 = o->state_bits == 8;
+    const size_t gsz = o->grad_dtype == SFB_BF16 ? 2 : 4, wide_state = bits8 ? 8 : 16;
+    for (int32_t i = 0; i < count; ++i) {
+        const sfb_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > kMostElements) return SFB_ESHAPE;
+        list[i] = AdamwTensor{t.p, t.g, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, 0, 0};
+        if (t.n == 0) continue;
+        if (!t.p || !t.g || !t.m || !t.v || (bits8 && (!t.m_scale || !t.v_scale))) return SFB_EINVAL;
+        if (!aligned(t.p, 4) || !aligned(t.g, gsz) || (!bits8 && (!aligned(t.m, 4) || !aligned(t.v, 4))) || !aligned(t.copy, 2)) return SFB_EINVAL;
+        list[i].wide = aligned(t.p, 16) && aligned(t.g, 16) && aligned(t.m, wide_state) && aligned(t.v, wide_state) && aligned(t.copy, 16);
+    }
+    AdamwRates r{};
+    r.lr = o->lr; r.eps = o->eps; r.decay = o->weight_decay;
+    r.beta1 = o->beta1; r.beta2 = o->beta2;
+    r.one_beta1 = (float)(1.0 - (double)o->beta1); r.one_beta2 = (float)(1.0 - (double)o->beta2);
+    r.log_beta1 = std::log((double)o->beta1); r.log_beta2 = std::log((double)o->beta2);
+    r.seed = o->seed; r.step = o->step; r.grad_scale = o->grad_scale; r.lr_scale = o->lr_scale;
+    OnDevice on(c);
+    Timed t(c, 7);
+    hipError_t e = launch_adamw(list.data(), count, r, o->grad_dtype == SFB_BF16, o->state_bits, c->stream);
+    if (e != hipSuccess) return hip_fail(c, e);
+    return SFB_OK;
+}
+
+sfb_status sfb_adamw_unpack(sfb_ctx* c, const sfb_adamw_tensor* tensors, int32_t count, void* const* m_out, void* const* v_out) {
+    if (!c || count < 0 || (count > 0 && (!tensors || !m_out || !v_out))) return SFB_EINVAL;
+    std::vector<AdamwTensor> list;
+    try {
+        list.resize((size_t)count);
+    } catch (...) {
+        return SFB_EINVAL;
+    }
+    for (int32_t i = 0; i < count; ++i) {
+        const sfb_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > kMostElements) return SFB_ESHAPE;
+        list[i] = AdamwTensor{(float*)m_out[i], nullptr, t.m, t.v, t.m_scale, t.v_scale, v_out[i], t.n, 0, 0};
+        if (t.n == 0) continue;
+        if (!t.m || !t.v || !t.m_scale || !t.v_scale || !m_out[i] || !v_out[i]) return SFB_EINVAL;
+        if (!aligned(m_out[i], 2) || !aligned(v_out[i], 2)) return SFB_EINVAL;
+        list[i].wide = aligned(t.m, 8) && aligned(t.v, 8) && aligned(m_out[i], 16) && aligned(v_out[i], 16);
+    }
+    OnDevice on(c);
+    hipError_t e = launch_adamw_unpack(list.data(), count, c->stream);
+    if (e != hipSuccess) return hip_fail(c, e);
+    return SFB_OK;
+}
+
+static sfb_status grad_list(const sfb_gradient* grads, int32_t count, size_t gsz, std::vector<GradTensor>* list) {
+    if (count < 0 || (count > 0 && !grads)) return SFB_EINVAL;
+    try {
+        list->resize((size_t)count);
+    } catch (...) {
+        return SFB_EINVAL;
+    }
+    for (int32_t i = 0; i < count; ++i) {
+        if (grads[i].n < 0 || grads[i].n > kMostElements) return SFB_ESHAPE;
+        if (grads[i].n > 0 && (!grads[i].g || !aligned(grads[i].g, gsz))) return SFB_EINVAL;
+        (*list)[i] = GradTensor{grads[i].g, grads[i].n, aligned(grads[i].g, 16)};
+    }
+    return SFB_OK;
+}
+
+sfb_status sfb_grad_norm_bytes(const sfb_gradient* grads, int32_t count, size_t* bytes) {
+    if (!bytes) return SFB_EINVAL;
+    std::vector<GradTensor> list;
+    sfb_status s = grad_list(grads, count, 1, &list);
+    if (s != SFB_OK) return s;
+    *bytes = (size_t)(grad_norm_chunks(list.data(), count) + 1) * sizeof(double);
+    return SFB_OK;
+}
+
+sfb_status sfb_grad_norm(sfb_ctx* c, const sfb_gradient* grads, int32_t count, sfb_dtype grad_dtype, float max_norm, float* out, void* ws,
+                         size_t ws_bytes) {
+    if (!c || !out || !(max_norm > 0.f)) return SFB_EINVAL;
+    if (grad_dtype != SFB_F32 && grad_dtype != SFB_BF16) return SFB_EDTYPE;
+    std::vector<GradTensor> list;
+    sfb_status s = grad_list(grads, count, grad_dtype == SFB_BF16 ? 2 : 4, &list);
+    if (s != SFB_OK) return s;
+    if (!ws || !aligned(ws, 8) || ws_bytes < (size_t)(grad_norm_chunks(list.data(), count) + 1) * sizeof(double)) return SFB_EWORKSPACE;
+    OnDevice on(c);
+    Timed t(c, 7);
+    hipError_t e = launch_grad_norm(list.data(), count, grad_dtype == SFB_BF16, max_norm, out, (double*)ws, c->stream);
+    if (e != hipSuccess) return hip_fail(c, e);
     return SFB_OK;
 }
 

@@ -313,4 +313,33 @@ size_t fused_extra_workspace(int64_t D, int64_t N);
 bool fused_call_ok(const FusedArgs& a);   // alignment and size of this call's operands
 hipError_t launch_fused(const FusedArgs& a, const FusedPlan& p, void* ws_factors, void* ws_next, hipStream_t s);
 
+// AdamW over many tensors and the norm of many gradients (sfb_adamw.hip).
+constexpr int kAdamwTensors = 44, kGradTensors = 128;    // of a launch: their table travels in its arguments (4 KB)
+struct AdamwTensor {
+    float* p;
+    const void* g;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;     // 8-bit moments only
+    void* copy;                     // bf16 copy of p, or nullptr
+    int64_t n;
+    int64_t first;                  // blocks of 128 elements before this tensor (set by the launcher)
+    int32_t wide;                   // every pointer is aligned for eight elements at a time
+};
+struct AdamwRates {
+    float lr, eps, decay, beta1, beta2, one_beta1, one_beta2;
+    uint32_t seed;
+    double log_beta1, log_beta2;
+    int32_t* step;
+    const float *grad_scale, *lr_scale;
+};
+hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwRates& r, bool bf16_grads, int bits, hipStream_t s);
+hipError_t launch_adamw_unpack(const AdamwTensor* t, int count, hipStream_t s);   // m to p, v to copy, both bf16
+struct GradTensor {
+    const void* g;
+    int64_t n;
+    int32_t wide;
+};
+int64_t grad_norm_chunks(const GradTensor* t, int count);                          // doubles of workspace
+hipError_t launch_grad_norm(const GradTensor* t, int count, bool bf16, float max_norm, float* out, double* partial, hipStream_t s);
+
 }  // namespace sfb
