@@ -296,6 +296,56 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
                          const uint8_t *active, sfb_prox_kind kind, float param);
 
 /*
+ * Softmax cross entropy of a linear head over a large vocabulary (SFB_MLR contexts: J words, D features, features in the context's
+ * dtype, up to P*B rows a call), with the gradients by the features and by W, and without the n x J scores or factors in memory:
+ * what sfb_compute_factors keeps as Z and U is formed in pieces of the vocabulary and used at once.  With z_i = W a_i:
+ *     lse_i = log sum_j exp(z_ij)       loss_i = lse_i - z_i,y(i)       total = sum_i f w_i loss_i
+ *     u_ij = f w_i (exp(z_ij - lse_i) - [j = y(i)])       dA = U W  [n][D]       dW = U^T A  [J][D]
+ * with w_i = weight[i] or 1, and f = scale, or scale divided by the number of rows that take part (mean != 0).  A row whose label lies outside
+ * [0, J) takes no part: its loss, lse and row of dA are 0, and its features are not looked at (they may be anything).  Rows n and
+ * beyond of no output are touched; n = 0 is an empty batch (total = 0, dW = 0).
+ *   W, a        each in its own dtype: bf16 products are taken as they are, fp32 operands as three bf16 terms (exact below 3.38e38; what is
+ *               beyond, or below 2^-109 in part, is rounded to bf16's range), sums in fp32
+ *   dA, dW      in the types of a and W, or NULL: not wanted.  With both in bf16 U is rounded to bf16 on the way (as large an error again as the
+ *               results' own rounding); otherwise it is kept in three terms
+ *   loss, lse, total, weight   DEVICE fp32, NULL: not wanted (lse is needed by sfb_xent_gradients, which reads what sfb_xent_loss left)
+ *   ws          DEVICE, 256-byte aligned; it belongs to the call until that has run: calls that may overlap in time, replays of captured
+ *               ones included, need one each.  sfb_xent_workspace_bytes: the least a call on up to P*B rows can take, and as much as
+ *               speeds it up (pieces of some 256 MB).  grads != 0: of the calls that form gradients.
+ * sfb_xent_gradients and sfb_xent_loss_and_gradients give the same gradients, to rounding.  Results do not depend on the order in which
+ * anything runs.  No two of the arrays may overlap.
+ * SFB_EINVAL: a null pointer that is needed, a scale that is not finite, ws not aligned; SFB_ESHAPE: a leading dimension shorter than a row, n outside
+ * [0, P*B]; SFB_EDTYPE; SFB_EUNSUPPORTED: not an SFB_MLR context, D beyond 2^22; SFB_EWORKSPACE.  Nothing is launched if an argument is refused.
+ * Timed under family 8 (the first product of a call).
+ */
+typedef struct sfb_xent {
+    const void *W;               /* [J][ldw] */
+    int64_t ldw;
+    sfb_dtype w_dtype;
+    int32_t mean;
+    const void *a;               /* [n][lda] */
+    int64_t lda;
+    const int32_t *y;            /* [n] */
+    int64_t n;
+    float *loss;                 /* [n] */
+    float *lse;                  /* [n] */
+    float *total;                /* [1] */
+    const float *weight;         /* [n] */
+    float scale;
+    int32_t reserved;            /* 0 */
+    void *dA;                    /* [n][ldda] */
+    int64_t ldda;
+    void *dW;                    /* [J][lddw] */
+    int64_t lddw;
+    void *ws;
+    size_t ws_bytes;
+} sfb_xent;
+SFB_API sfb_status sfb_xent_workspace_bytes(const sfb_ctx *ctx, sfb_dtype w_dtype, int32_t grads, size_t *least, size_t *best);
+SFB_API sfb_status sfb_xent_loss(sfb_ctx *ctx, const sfb_xent *x);
+SFB_API sfb_status sfb_xent_gradients(sfb_ctx *ctx, const sfb_xent *x);
+SFB_API sfb_status sfb_xent_loss_and_gradients(sfb_ctx *ctx, const sfb_xent *x);
+
+/*
  * AdamW over many tensors at once, an alternative to W <- W - eta dW with moments of the gradient.  With g' = grad_scale * g,
  * t the step being taken (the first is 1):
  *     m <- beta1 m + (1 - beta1) g'         v <- beta2 v + (1 - beta2) g'^2
@@ -383,8 +433,8 @@ SFB_API int sfb_last_hip_error(const sfb_ctx *ctx);
  * (0 = scores, or the one-pass kernel of few classes, without the kernel that adds its planes; 1 = factor u, 2 =
  * reconstruct-apply: the contraction, without the kernels that pack bf16 operands, copy ragged factors, make the stored
  * entries' lists or add planes, 3 = CSR densify / stream copy, 4 = proximal step, 5 = the one-pass update +
- * next scores kernel of sfb_step_pipelined, without its packing kernel, 7 = AdamW and gradient norms, the first launch of
- * a call) since the last reset.
+ * next scores kernel of sfb_step_pipelined, without its packing kernel, 7 = AdamW and gradient norms, 8 = cross entropy of a
+ * head, the first launch of a call in both; 6 is none) since the last reset.
  */
 SFB_API sfb_status sfb_plan_info(const sfb_ctx *ctx, int32_t *fwd_split_k, int32_t *fwd_grid,
                          int32_t *recon_grid);

@@ -9,4 +9,5 @@ from .binding import (  # noqa: F401
     SFB_MLR, SFB_DML, SFB_L2SVM, SFB_F32, SFB_BF16, SfbError, SfbBatch, Sfb, SspSimulator, halton_receivers, lib, library_path,
     sfb_strerror,
 )
+from .head import SoftmaxHead  # noqa: F401
 from .optim import AdamW, GradNorm  # noqa: F401

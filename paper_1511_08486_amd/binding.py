@@ -43,6 +43,13 @@ class sfb_adamw(C.Structure):
                 ("grad_scale", C.c_void_p), ("lr_scale", C.c_void_p)]
 
 
+class sfb_xent(C.Structure):
+    _fields_ = [("W", C.c_void_p), ("ldw", C.c_int64), ("w_dtype", C.c_int), ("mean", C.c_int32), ("a", C.c_void_p), ("lda", C.c_int64),
+                ("y", C.c_void_p), ("n", C.c_int64), ("loss", C.c_void_p), ("lse", C.c_void_p), ("total", C.c_void_p),
+                ("weight", C.c_void_p), ("scale", C.c_float), ("reserved", C.c_int32), ("dA", C.c_void_p), ("ldda", C.c_int64),
+                ("dW", C.c_void_p), ("lddw", C.c_int64), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
 class sfb_gradient(C.Structure):
     _fields_ = [("g", C.c_void_p), ("n", C.c_int64)]
 
@@ -90,6 +97,10 @@ def _load():
         "sfb_prox": (C.c_int, [vp, vp, i64, C.c_int, f32, f32]),
         "sfb_reconstruct_apply_prox": (C.c_int, [vp, vp, i64, vp, i64, vp, i64, f32, f32, vp, C.c_int, f32]),
         "sfb_step_prox": (C.c_int, [vp, vp, i64, pb, vp, vp, i64, vp, i64, vp, f32, vp, C.c_int, f32]),
+        "sfb_xent_workspace_bytes": (C.c_int, [vp, C.c_int, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+        "sfb_xent_loss": (C.c_int, [vp, C.POINTER(sfb_xent)]),
+        "sfb_xent_gradients": (C.c_int, [vp, C.POINTER(sfb_xent)]),
+        "sfb_xent_loss_and_gradients": (C.c_int, [vp, C.POINTER(sfb_xent)]),
         "sfb_adamw_step": (C.c_int, [vp, C.POINTER(sfb_adamw_tensor), i32, C.POINTER(sfb_adamw)]),
         "sfb_adamw_unpack": (C.c_int, [vp, C.POINTER(sfb_adamw_tensor), i32, C.POINTER(vp), C.POINTER(vp)]),
         "sfb_grad_norm_bytes": (C.c_int, [C.POINTER(sfb_gradient), i32, C.POINTER(C.c_size_t)]),

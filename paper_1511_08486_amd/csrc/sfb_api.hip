@@ -1045,10 +1045,64 @@ sfb_status sfb_reset_timing(sfb_ctx* c) {
     return SFB_OK;
 }
 
+static bool aligned(const void* p, size_t to) { return ((uintptr_t)p % to) == 0; }
+
+// ---- softmax cross entropy of a head -----------------------------------------------------------------------------
+
+sfb_status sfb_xent_workspace_bytes(const sfb_ctx* c, sfb_dtype w_dtype, int32_t grads, size_t* least, size_t* best) {
+    if (!c || (!least && !best)) return SFB_EINVAL;
+    if (w_dtype != SFB_F32 && w_dtype != SFB_BF16) return SFB_EDTYPE;
+    if (c->model != SFB_MLR || c->D > (1 << 22)) return SFB_EUNSUPPORTED;
+    XentCall x{};
+    x.w_bf16 = w_dtype == SFB_BF16; x.a_bf16 = c->dtype == SFB_BF16;
+    x.n = (int64_t)c->P * c->B; x.J = c->J; x.D = c->D;
+    if (least) *least = xent_workspace(x, grads != 0, true);
+    if (best) *best = xent_workspace(x, grads != 0, false);
+    return SFB_OK;
+}
+
+static sfb_status run_xent(sfb_ctx* c, const sfb_xent* x, bool forward, bool grads) {
+    if (!c || !x || !x->W || !std::isfinite(x->scale)) return SFB_EINVAL;
+    if (x->w_dtype != SFB_F32 && x->w_dtype != SFB_BF16) return SFB_EDTYPE;
+    if (c->model != SFB_MLR || c->D > (1 << 22)) return SFB_EUNSUPPORTED;
+    if (x->n < 0 || x->n > (int64_t)c->P * c->B) return SFB_ESHAPE;
+    if (x->n > 0 && (!x->a || !x->y || (!forward && !x->lse))) return SFB_EINVAL;
+    if (x->ldw < c->D || (x->n > 0 && x->lda < c->D)) return SFB_ESHAPE;
+    const size_t wsz = x->w_dtype == SFB_BF16 ? 2 : 4, asz = c->dtype == SFB_BF16 ? 2 : 4;
+    if (!aligned(x->W, wsz) || !aligned(x->a, asz)) return SFB_EINVAL;
+    if (grads) {
+        if (x->dA && (x->ldda < c->D)) return SFB_ESHAPE;
+        if (x->dW && (x->lddw < c->D)) return SFB_ESHAPE;
+        if (!aligned(x->dA, asz) || !aligned(x->dW, wsz)) return SFB_EINVAL;
+    }
+    XentCall k{};
+    k.W = x->W; k.ldw = x->ldw; k.w_bf16 = x->w_dtype == SFB_BF16;
+    k.a = x->a; k.lda = x->lda; k.a_bf16 = c->dtype == SFB_BF16;
+    k.y = x->y; k.n = x->n; k.J = c->J; k.D = c->D;
+    k.loss = x->loss; k.lse = x->lse; k.total = x->total; k.weight = x->weight;
+    k.scale = x->scale; k.mean = x->mean;
+    k.dA = x->dA; k.ldda = x->ldda; k.dW = x->dW; k.lddw = x->lddw;
+    k.ws = x->ws; k.ws_bytes = x->ws_bytes;
+    if (x->ws && !aligned(x->ws, 256)) return SFB_EINVAL;
+    grads = grads && (x->dA || x->dW);
+    XentCall most = k;                                                   // the bound does not depend on this call's rows and alignment
+    most.n = (int64_t)c->P * c->B;
+    if (!x->ws || x->ws_bytes < xent_workspace(most, grads, true)) return SFB_EWORKSPACE;
+    if (!forward && !grads) return SFB_OK;                               // nothing is wanted
+    OnDevice on(c);
+    Timed t(c, 8);
+    hipError_t e = launch_xent(k, forward, grads, c->stream);
+    if (e != hipSuccess) return hip_fail(c, e);
+    return SFB_OK;
+}
+
+sfb_status sfb_xent_loss(sfb_ctx* c, const sfb_xent* x) { return run_xent(c, x, true, false); }
+sfb_status sfb_xent_gradients(sfb_ctx* c, const sfb_xent* x) { return run_xent(c, x, false, true); }
+sfb_status sfb_xent_loss_and_gradients(sfb_ctx* c, const sfb_xent* x) { return run_xent(c, x, true, true); }
+
 // ---- AdamW over many tensors, the norm of many gradients ---------------------------------------------------------
 
 static constexpr int64_t kMostElements = 1LL << 40;
-static bool aligned(const void* p, size_t to) { return ((uintptr_t)p % to) == 0; }
 
 sfb_status sfb_adamw_step(sfb_ctx* c, const sfb_adamw_tensor* tensors, int32_t count, const sfb_adamw* o) {
     if (!c || !o || count < 0 || (count > 0 && !tensors) || !o->step) return SFB_EINVAL;

@@ -342,4 +342,26 @@ struct GradTensor {
 int64_t grad_norm_chunks(const GradTensor* t, int count);                          // doubles of workspace
 hipError_t launch_grad_norm(const GradTensor* t, int count, bool bf16, float max_norm, float* out, double* partial, hipStream_t s);
 
+// Softmax cross entropy of a linear head without the scores in memory, and its gradients (sfb_xent.hip).
+struct XentCall {
+    const void* W;
+    int64_t ldw;
+    bool w_bf16;
+    const void* a;
+    int64_t lda;
+    bool a_bf16;
+    const int32_t* y;
+    int64_t n, J, D;
+    float *loss, *lse, *total;
+    const float* weight;
+    float scale;
+    int mean;
+    void *dA, *dW;
+    int64_t ldda, lddw;
+    void* ws;
+    size_t ws_bytes;
+};
+size_t xent_workspace(const XentCall& c, bool grads, bool least);        // reads n, J, D and the types
+hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t s);
+
 }  // namespace sfb

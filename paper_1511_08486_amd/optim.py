@@ -12,14 +12,14 @@ from .binding import SFB_BF16, SFB_F32, SFB_MLR, SfbError, lib, sfb_adamw, sfb_a
 class _Stream:
     """An sfb_ctx that carries a stream for calls that need nothing else of it."""
 
-    def __init__(self, stream, device):
+    def __init__(self, stream, device, shape=(SFB_MLR, 1, 1, 1, 1, SFB_F32)):
         self.device = torch.device(device)
         if stream is None:
             stream = torch.cuda.current_stream(self.device).cuda_stream
         self.stream = int(stream)
         self._ctx = C.c_void_p()
         with torch.cuda.device(self.device):
-            self._check(lib.sfb_create(C.byref(self._ctx), SFB_MLR, 1, 1, 1, 1, SFB_F32, C.c_void_p(self.stream)), "sfb_create")
+            self._check(lib.sfb_create(C.byref(self._ctx), *shape, C.c_void_p(self.stream)), "sfb_create")
 
     def _check(self, status, where):
         if status != 0:
