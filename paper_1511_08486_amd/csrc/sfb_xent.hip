@@ -237,40 +237,32 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
         else xe_wait_barrier();
         const unsigned char* now = xe_lds;
         split_for<0, READS>([&](auto r) { read(I0, r, f0, now); });
-        // a stage: its last step is multiplied behind the barrier that frees its buffer, while the first of the next is read and
-        // the first half of the stage ST ahead requested; the other half during the next stage's first step
-        bool half_left = false;
-        auto stage = [&](auto more, auto steady) {
-            constexpr bool MORE = decltype(more)::value, STEADY = decltype(steady)::value;
-            if (half_left) {
-                phase(I1, I1, MID, ALL, f0, f1, now);
-                next();
-            } else {
-                phase(I1, I1, I0, I0, f0, f1, now);
-            }
+        // the last step of a stage is multiplied behind the barrier that frees its buffer, while the first of the next is read; the stage
+        // ST ahead is requested during that and the next step
+        phase(I1, I1, I0, I0, f0, f1, now);
+        phase(I2, I1, I0, I0, f1, f0, now);
+        phase(I3, I1, I0, I0, f0, f1, now);
+        auto follow = [&]() { now = now + STAGE == xe_lds + ST * STAGE ? xe_lds : now + STAGE; };
+        int s = 0;
+        for (; s + ST < stages; ++s) {
+            xe_stage_barrier<(ST - 2) * LOADS>();                        // the ST - 2 stages after the next may still be on their way
+            follow();
+            aim();
+            phase(I0, I1, I0, MID, f1, f0, now);
+            phase(I1, I1, MID, ALL, f0, f1, now);
+            next();
             phase(I2, I1, I0, I0, f1, f0, now);
             phase(I3, I1, I0, I0, f0, f1, now);
-            if constexpr (!MORE) {
-                phase(I0, I0, I0, I0, f1, f0, now);
-                return;
-            }
-            // STEADY: the ST - 2 stages after the next may still be on their way
-            if constexpr (STEADY) xe_stage_barrier<(ST - 2) * LOADS>();
-            else xe_wait_barrier();
-            const unsigned char* following = now + STAGE == xe_lds + ST * STAGE ? xe_lds : now + STAGE;
-            if constexpr (STEADY) {
-                aim();
-                phase(I0, I1, I0, MID, f1, f0, following);
-            } else {
-                phase(I0, I1, I0, I0, f1, f0, following);
-            }
-            half_left = STEADY;
-            now = following;
-        };
-        int s = 0;
-        for (; s + ST < stages; ++s) stage(std::true_type{}, std::true_type{});
-        for (; s + 1 < stages; ++s) stage(std::true_type{}, std::false_type{});
-        stage(std::false_type{}, std::false_type{});
+        }
+        for (; s + 1 < stages; ++s) {
+            xe_wait_barrier();
+            follow();
+            phase(I0, I1, I0, I0, f1, f0, now);
+            phase(I1, I1, I0, I0, f0, f1, now);
+            phase(I2, I1, I0, I0, f1, f0, now);
+            phase(I3, I1, I0, I0, f0, f1, now);
+        }
+        phase(I0, I0, I0, I0, f1, f0, now);
     }
     xe_wait_barrier();                                                   // LDS is free
 
