@@ -12,8 +12,13 @@
 // One kernel multiplies: out[n][m] = sum_k Y[n][k] X[m][k], operands in bf16 terms, m contiguous in memory; X and Y each lie with k
 // contiguous or with k as their slow index (gfx950's transposing LDS read takes those as they are).
 //   scores  X = W[j][d], Y = A[i][d]      dA  X = W[j][d] (k = j slow), Y = U[i][j]      dW  X = A[i][d], Y = U[i][j] (k = i slow, both)
-// fp32 operands are three bf16 terms each (exact), a product six of theirs; with one bf16 operand three.  They are a longer k to the
-// kernel: the small products first, so that the sum is rounded at its full size only along the last one.
+// fp32 operands go in terms of 16 bits, a longer k to the kernel, the small products first:
+//   scores and dA  two fp16 terms of every row divided by its own power of two, x = 2^e (h + l / 2048): 22 bits of every value above 2^-29 of its
+//                  row's largest, and three products (two with one bf16 operand, which is one fp16 term).  Of dA's contraction W's exponents
+//                  are in U, and U's rows are divided by what their factor g_i bounds them by.  A bf16 dA takes one term of each (2^-12).
+//   dW             three bf16 terms (exact) and six products (three with bf16 features): along its contraction, the rows, the factors of a
+//                  rare word may all be below 2^-40 of a label's, and must not be rounded by that.
+// Small problems, whose scores and U fit the workspace beside each other, keep the scores of the one piece instead of forming them twice.
 #include "sfb_kernels.h"
 #include "sfb_split.h"
 
@@ -31,6 +36,7 @@ struct XentProduct {
     int k_tiles, last_x, last_y;             // stages of one pair of terms; where the last one begins (k contiguous)
     int pairs;
     uint32_t pair_x, pair_y;                 // four bits a pair: the terms of X and Y, in order
+    const int *exp_m, *exp_n, *exp_top;      // fp16 terms: results are times 2^(exp_m[m] + exp_n[n] + *exp_top); null: 0
     int m_tiles, n_tiles, total, splits, per_split;
     const int* count;                        // rows that take part
     bool n_is_rows, k_is_rows;               // what `count` bounds
@@ -41,9 +47,10 @@ struct XentProduct {
     float* z_label;
     int ld_rows;
     const float *lse, *g;
-    bf16_t* u;                               // [terms][..][ldu]
+    bf16_t *u, *u16;                         // [terms][..][ldu], in bf16 and fp16
     int64_t ldu, u_plane;
-    int u_terms;
+    int u_terms, u16_terms;
+    const int *exp_g, *exp_words;            // U's fp16 terms are of u 2^(exp_m[m] - exp_g[n] - *exp_words)
     // kXeStore
     void* out;
     int64_t ldo, out_plane;                  // out_plane: between splits
@@ -126,7 +133,31 @@ __device__ __forceinline__ void xe_wait_barrier() { asm volatile("s_waitcnt vmcn
 template <int LEFT>
 __device__ __forceinline__ void xe_stage_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
 
-template <int WGM, int WGN, int MT, int NT, int ST, int OCC, bool XT, bool YT, int END, class Out>
+// fp16 terms of x[0..3], the second 2^11 times as large; x becomes what they leave
+__device__ __forceinline__ uint2 xe_half4(float (&x)[4]) {
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    const h4 h = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (x[e] - (float)h[e]) * 2048.f;
+    return __builtin_bit_cast(uint2, h);
+}
+__device__ __forceinline__ uint2 xe_bf4(float (&x)[4]) {
+    const uint2 w = make_uint2(cvt_pk_bf16(x[0], x[1]), cvt_pk_bf16(x[2], x[3]));
+    x[0] -= __uint_as_float(w.x << 16);
+    x[1] -= __uint_as_float(w.x & 0xffff0000u);
+    x[2] -= __uint_as_float(w.y << 16);
+    x[3] -= __uint_as_float(w.y & 0xffff0000u);
+    return w;
+}
+
+template <bool F16>
+__device__ __forceinline__ f32x16 xe_mfma(sp_u32x4 a, sp_u32x4 b, f32x16 c) {
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(sp_f16x8, a), __builtin_bit_cast(sp_f16x8, b), c, 0, 0, 0);
+    else return split_mfma(a, b, c);
+}
+
+// F16: operands in fp16 terms, exponents beside them; the products of a second term come first and are 2^11 times as large
+template <int WGM, int WGN, int MT, int NT, int ST, int OCC, bool XT, bool YT, bool F16, int END, class Out>
 __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const XentProduct a) {
     constexpr int WAVES = WGM * WGN, BM = WGM * MT * 32, BN = WGN * NT * 32;
     typedef XentSide<XT, BM, WAVES, MT> SideX;
@@ -214,7 +245,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
                 split_for<(R0 < READS ? R0 : READS), (R1 < READS ? R1 : READS)>([&](auto r) { read(sc, r, then, from); });
             }
             __builtin_amdgcn_sched_barrier(0);
-            acc[q / NT][q % NT] = split_mfma(now.x[q / NT], now.y[q % NT], acc[q / NT][q % NT]);
+            acc[q / NT][q % NT] = xe_mfma<F16>(now.x[q / NT], now.y[q % NT], acc[q / NT][q % NT]);
             __builtin_amdgcn_sched_barrier(0);
             split_for<FIRST + q * COUNT / MFMAS, FIRST + (q + 1) * COUNT / MFMAS>([&](auto i) { request(i); });
         });
@@ -242,6 +273,18 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
         phase(I1, I1, I0, I0, f0, f1, now);
         phase(I2, I1, I0, I0, f1, f0, now);
         phase(I3, I1, I0, I0, f0, f1, now);
+        // behind the last product of a second term
+        const int shrink_at = F16 && a.pairs > 1 ? (k_end - k_begin) * (a.pairs - 1) - 1 : -1;
+        auto shrink = [&](int s) {
+            if constexpr (F16) {
+                if (s == shrink_at) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] *= 1.f / 2048.f;
+                }
+            }
+        };
         auto follow = [&]() { now = now + STAGE == xe_lds + ST * STAGE ? xe_lds : now + STAGE; };
         int s = 0;
         for (; s + ST < stages; ++s) {
@@ -249,6 +292,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
             follow();
             aim();
             phase(I0, I1, I0, MID, f1, f0, now);
+            shrink(s);
             phase(I1, I1, MID, ALL, f0, f1, now);
             next();
             phase(I2, I1, I0, I0, f1, f0, now);
@@ -258,6 +302,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
             xe_wait_barrier();
             follow();
             phase(I0, I1, I0, I0, f1, f0, now);
+            shrink(s);
             phase(I1, I1, I0, I0, f0, f1, now);
             phase(I2, I1, I0, I0, f1, f0, now);
             phase(I3, I1, I0, I0, f0, f1, now);
@@ -267,6 +312,27 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
     xe_wait_barrier();                                                   // LDS is free
 
     const int mw = m0 + wm * MT * 32 + 4 * half, nw = n0 + wn * NT * 32 + l32;      // entry e of (i, j): m = mw + 32 i + 8 (e / 4) + e % 4
+    // exponents of four m from mw + 32 i + 8 q on (the arrays reach to the end of the last tile)
+    auto exps_of = [&](int i, int q) { return *reinterpret_cast<const int4*>(a.exp_m + mw + 32 * i + 8 * q); };
+    if constexpr (F16) {
+        const int top = a.exp_top ? *a.exp_top : 0;
+        int en[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) en[j] = top + (a.exp_n && nw + 32 * j < count ? a.exp_n[nw + 32 * j] : 0);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int4 em = a.exp_m ? exps_of(i, q) : make_int4(0, 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    acc[i][j][4 * q] = __builtin_ldexpf(acc[i][j][4 * q], en[j] + em.x);
+                    acc[i][j][4 * q + 1] = __builtin_ldexpf(acc[i][j][4 * q + 1], en[j] + em.y);
+                    acc[i][j][4 * q + 2] = __builtin_ldexpf(acc[i][j][4 * q + 2], en[j] + em.z);
+                    acc[i][j][4 * q + 3] = __builtin_ldexpf(acc[i][j][4 * q + 3], en[j] + em.w);
+                }
+            }
+    }
     if constexpr (END == kXeStats) {
         float2* const red = reinterpret_cast<float2*>(xe_lds);
         const bool inside = m0 + BM <= a.M;
@@ -327,37 +393,52 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
                     acc[i][j][e] = real && (inside || mw + m < a.M) ? u : 0.f;
                 }
         }
-        for (int term = 0; term < a.u_terms; ++term) {
-            if (term > 0) __syncthreads();
+        // the tile of one term: to LDS by columns of m, to memory by rows of n.  term_of(x, i, j, q): its bits of the four values x
+        auto pass_on = [&](bf16_t* to, auto term_of) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int row = wn * NT * 32 + 32 * j + l32;
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int q = 0; q < 4; ++q) {
+                    const int4 em = F16 ? exps_of(i, q) : make_int4(0, 0, 0, 0);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint2 w;
-                        w.x = cvt_pk_bf16(acc[i][j][4 * q], acc[i][j][4 * q + 1]);
-                        w.y = cvt_pk_bf16(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                        // what the term leaves over, exact
-                        acc[i][j][4 * q] -= __uint_as_float(w.x << 16);
-                        acc[i][j][4 * q + 1] -= __uint_as_float(w.x & 0xffff0000u);
-                        acc[i][j][4 * q + 2] -= __uint_as_float(w.y << 16);
-                        acc[i][j][4 * q + 3] -= __uint_as_float(w.y & 0xffff0000u);
+                    for (int j = 0; j < NT; ++j) {
+                        const int row = wn * NT * 32 + 32 * j + l32;
+                        float x[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * q + e];
+                        const uint2 w = term_of(x, em, j);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = x[e];
                         const int piece = (wm * MT * 32 + 32 * i + 8 * q) / 8;
                         *reinterpret_cast<uint2*>(xe_lds + row * (BM * 2) + ((piece ^ (row & 15)) << 4) + 8 * half) = w;
                     }
-            }
+                }
             __syncthreads();
-            bf16_t* const u = a.u + term * a.u_plane + m0;
+            to += m0;
             for (int c = tid; c < BN * PER; c += WAVES * 64) {
                 const int row = c / PER, piece = c % PER;
-                *reinterpret_cast<sp_u32x4*>(u + (int64_t)(n0 + row) * a.ldu + piece * 8) =
+                *reinterpret_cast<sp_u32x4*>(to + (int64_t)(n0 + row) * a.ldu + piece * 8) =
                     *reinterpret_cast<const sp_u32x4*>(xe_lds + row * (BM * 2) + ((piece ^ (row & 15)) << 4));
                 // dW takes whole stages of 64 rows
-                if constexpr (BN == 32) *reinterpret_cast<sp_u32x4*>(u + (int64_t)(n0 + 32 + row) * a.ldu + piece * 8) = sp_u32x4{0u, 0u, 0u, 0u};
+                if constexpr (BN == 32) *reinterpret_cast<sp_u32x4*>(to + (int64_t)(n0 + 32 + row) * a.ldu + piece * 8) = sp_u32x4{0u, 0u, 0u, 0u};
+            }
+            __syncthreads();
+        };
+        if constexpr (F16) {
+            if (a.u16_terms > 0) {
+                int en[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) en[j] = nw + 32 * j < count ? -a.exp_g[nw + 32 * j] - *a.exp_words : 0;
+                for (int term = 0; term < a.u16_terms; ++term)
+                    pass_on(a.u16 + term * a.u_plane, [&](float(&x)[4], int4 em, int j) {
+                        float y[4] = {__builtin_ldexpf(x[0], en[j] + em.x), __builtin_ldexpf(x[1], en[j] + em.y), __builtin_ldexpf(x[2], en[j] + em.z),
+                                      __builtin_ldexpf(x[3], en[j] + em.w)};
+                        const uint2 h = xe_half4(y);
+                        return term == 0 ? h : xe_half4(y);
+                    });
             }
         }
+        for (int term = 0; term < a.u_terms; ++term) pass_on(a.u + term * a.u_plane, [](float(&x)[4], int4, int) { return xe_bf4(x); });
     } else {
         // rows of n, as many 32-row blocks of every wavefront at a time as LDS holds in fp32
         constexpr int FIT = ST * STAGE / (WGN * 32 * BM * 4), JR = FIT < NT ? FIT : NT;
@@ -424,7 +505,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
 // One workgroup: the rows that take part, in order, then the others; label and factor of each of the former.
 __global__ __launch_bounds__(1024) void xent_rows_kernel(const int32_t* __restrict__ y, int n, int J, const float* __restrict__ weight, float scale,
                                                          int mean, int* __restrict__ rows, int* __restrict__ label, float* __restrict__ g,
-                                                         int* __restrict__ count) {
+                                                         int* __restrict__ exp_g, int* __restrict__ count) {
     __shared__ int before[16], total;
     int taken = 0;                                                       // so far, the same in every thread
     for (int base = 0; base < n; base += 1024) {
@@ -454,13 +535,16 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(const int32_t* __restri
         taken = total;
         __syncthreads();
     }
-    if (mean && taken > 0)
-        for (int k = threadIdx.x; k < taken; k += 1024) g[k] = g[k] / (float)taken;      // (written before the last barrier)
+    for (int k = threadIdx.x; k < taken; k += 1024) {                    // (written before the last barrier)
+        const float x = mean ? g[k] / (float)taken : g[k];
+        g[k] = x;
+        exp_g[k] = (int)(__float_as_uint(x) >> 23 & 255u) - 127 - 14;    // |u| <= |g| is below 2^15 of it
+    }
     if (threadIdx.x == 0) *count = taken;
 }
 
 // Rows of `src` in bf16 terms, k padded with zeros to whole stages.  rows: row of src for every packed row (the first *count of them; a row
-// behind those takes its results' zeros here), or nullptr: rows first .. first + n - 1.  window: one stage more that repeats the last 64
+// behind those takes its results' zeros here), or nullptr: rows 0 .. n - 1.  window: one stage more that repeats the last 64
 // columns of src, with zeros where they are in the stage before: it meets W's last 64 columns where W is read as it is.
 template <class T>
 __global__ __launch_bounds__(256) void xent_pack_kernel(const T* __restrict__ src, int64_t ld, int D, const int* __restrict__ rows,
@@ -499,6 +583,161 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(const T* __restrict__ sr
             x[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
         }
         *reinterpret_cast<sp_u32x4*>(dst + t * plane + (int64_t)k * ldd + p * 8) = w;
+    }
+}
+
+// Four elements of a row from d on, zeros from D on
+template <class T>
+__device__ __forceinline__ f32x4 xe_row4(const T* __restrict__ row, int d, int D) { return load4(row, d, D); }
+
+// Rows of `src` in fp16 terms: a workgroup a row, divided by 2^(exps[row]) so that its largest finite magnitude lies in [2^14, 2^15).
+// rows, count as above.
+template <class T>
+__global__ __launch_bounds__(256) void xent_pack16_kernel(const T* __restrict__ src, int64_t ld, int D, const int* __restrict__ rows,
+                                                          const int* __restrict__ count, int n, bf16_t* __restrict__ dst, int64_t ldd, int64_t plane,
+                                                          int terms, int* __restrict__ exps) {
+    __shared__ float part[4];
+    const int k = blockIdx.x, tid = threadIdx.x;
+    const int real = rows ? min(*count, n) : n;
+    bf16_t* const out = dst + (int64_t)k * ldd;
+    if (k >= real) {
+        for (int d = tid * 4; d < ldd; d += 1024)
+            for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = make_uint2(0u, 0u);
+        if (tid == 0) exps[k] = -200;                                    // below any other: has no say in the largest
+        return;
+    }
+    const T* const row = src + (int64_t)(rows ? rows[k] : k) * ld;
+    float top = 0.f;
+    for (int d = tid * 4; d < D; d += 1024) {
+        const f32x4 x = xe_row4(row, d, D);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.f);
+    }
+    top = wave_max(top);
+    if ((tid & 63) == 0) part[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    const int e0 = (int)(__float_as_uint(top) >> 23) - 127 - 14;         // (a row of zeros or of numbers below 2^-126: as if of those)
+    if (tid == 0) exps[k] = e0;
+    for (int d = tid * 4; d < ldd; d += 1024) {
+        const f32x4 v = xe_row4(row, d, D);
+        float x[4] = {__builtin_ldexpf(v[0], -e0), __builtin_ldexpf(v[1], -e0), __builtin_ldexpf(v[2], -e0), __builtin_ldexpf(v[3], -e0)};
+        for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = xe_half4(x);
+    }
+}
+
+// The largest of a piece's exponents
+__global__ __launch_bounds__(1024) void xent_top_kernel(const int* __restrict__ exps, int n, int* __restrict__ top) {
+    __shared__ int part[16];
+    int m = -200;
+    for (int i = threadIdx.x; i < n; i += 1024) m = max(m, exps[i]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o, kWave));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w) m = max(m, part[w]);
+        *top = m;
+    }
+}
+
+struct XentRows {
+    const float* z;                          // [splits][..][ldz] scores of the one piece
+    int64_t ldz, z_plane;
+    int splits, words, columns;              // columns: to the end of U's rows
+    const int *rows, *label, *count;
+    const float* g;
+    float *loss, *lse;
+    float* loss_packed;
+    float* lse_packed;
+    bf16_t *u, *u16;
+    int64_t ldu, u_plane;
+    int u_terms, u16_terms;
+    const int *exp_m, *exp_g, *exp_words;
+    bool given;                              // lse_packed is there already
+};
+constexpr int kXeRowThreads = 512;
+
+// Kept scores: a workgroup a row, loss and U from one row of scores (read again for U: it is in the die's cache by then)
+__global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows a) {
+    __shared__ float red[2][kXeRowThreads / 64], z_label;
+    const int k = blockIdx.x, tid = threadIdx.x, count = *a.count;
+    bf16_t* const u = a.u + (int64_t)k * a.ldu;
+    bf16_t* const u16 = a.u16 + (int64_t)k * a.ldu;
+    if (k >= count) {                                                    // dW takes whole stages of 64 rows
+        if (k < (count + 63) / 64 * 64)
+            for (int j = tid * 4; j < a.columns; j += kXeRowThreads * 4)
+                for (int t = 0; t < a.u_terms; ++t) *reinterpret_cast<uint2*>(u + t * a.u_plane + j) = make_uint2(0u, 0u);
+        return;
+    }
+    const float* const z = a.z + (int64_t)k * a.ldz;
+    auto scores = [&](int j) {                                           // four from j on; rows are padded to whole accesses
+        f32x4 s = *reinterpret_cast<const f32x4*>(z + j);
+        for (int p = 1; p < a.splits; ++p) s += *reinterpret_cast<const f32x4*>(z + p * a.z_plane + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = j + e < a.words ? s[e] : -__builtin_inff();
+        return s;
+    };
+    const int label = a.label[k];
+    float lse;
+    if (a.given) {
+        lse = a.lse_packed[k];
+    } else {
+        float top = -__builtin_inff(), sum = 0.f;
+        for (int j = tid * 4; j < a.words; j += kXeRowThreads * 4) {
+            const f32x4 s = scores(j);
+            const float m = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), top), base = m == -__builtin_inff() ? 0.f : m;
+            sum *= xe_exp(top - base);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum += xe_exp(s[e] - base);
+                if (j + e == label) z_label = s[e];
+            }
+            top = m;
+        }
+        const float m = wave_max(top);
+        sum = wave_sum(sum * xe_exp(top - (m == -__builtin_inff() ? 0.f : m)));
+        if ((tid & 63) == 0) {
+            red[0][tid >> 6] = m;
+            red[1][tid >> 6] = sum;
+        }
+        __syncthreads();
+        float most = red[0][0];
+#pragma unroll
+        for (int w = 1; w < kXeRowThreads / 64; ++w) most = fmaxf(most, red[0][w]);
+        const float base = most == -__builtin_inff() ? 0.f : most;
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kXeRowThreads / 64; ++w) sum += red[1][w] * xe_exp(red[0][w] - base);
+        const float l = logf(sum);
+        lse = most + l;
+        if (tid == 0) {
+            const float f = l + (most - z_label);
+            const int i = a.rows[k];
+            if (a.lse) a.lse[i] = lse;
+            if (a.loss) a.loss[i] = f;
+            a.loss_packed[k] = f;
+        }
+    }
+    const float g = a.g[k];
+    const int en = a.u16_terms > 0 ? -a.exp_g[k] - *a.exp_words : 0;
+    for (int j = tid * 4; j < a.columns; j += kXeRowThreads * 4) {
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        if (j < a.words) {
+            const f32x4 s = scores(j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = xe_exp(s[e] - lse);
+                if (j + e == label) x[e] -= 1.f;
+                x[e] = j + e < a.words ? x[e] * g : 0.f;
+            }
+        }
+        if (a.u16_terms > 0) {
+            const int4 em = *reinterpret_cast<const int4*>(a.exp_m + j);
+            float y[4] = {__builtin_ldexpf(x[0], en + em.x), __builtin_ldexpf(x[1], en + em.y), __builtin_ldexpf(x[2], en + em.z), __builtin_ldexpf(x[3], en + em.w)};
+            for (int t = 0; t < a.u16_terms; ++t) *reinterpret_cast<uint2*>(u16 + t * a.u_plane + j) = xe_half4(y);
+        }
+        for (int t = 0; t < a.u_terms; ++t) *reinterpret_cast<uint2*>(u + t * a.u_plane + j) = xe_bf4(x);
     }
 }
 
@@ -568,12 +807,12 @@ __global__ __launch_bounds__(256) void xent_rows_out_kernel(const float* __restr
 // ---------------------------------------------------------------------------------------------------------------
 // Plans and launches
 
-template <int WGM, int WGN, int MT, int NT, int ST, int OCC, bool XT, bool YT, int END, class Out>
-static hipError_t launch_product(XentProduct a, hipStream_t s) {
+template <int WGM, int WGN, int MT, int NT, int ST, int OCC, bool XT, bool YT, bool F16, int END, class Out>
+static hipError_t launch_tiles(XentProduct a, hipStream_t s) {
     constexpr int BM = WGM * MT * 32, BN = WGN * NT * 32;
     constexpr size_t lds = (size_t)ST * (BM + BN) * 128;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    auto* const kernel = &xent_product_kernel<WGM, WGN, MT, NT, ST, OCC, XT, YT, END, Out>;
+    auto* const kernel = &xent_product_kernel<WGM, WGN, MT, NT, ST, OCC, XT, YT, F16, END, Out>;
     if constexpr (lds > 64 * 1024) {
         static std::atomic<uint64_t> raised{0};                          // GPUs that know
         int dev = 0;
@@ -589,35 +828,57 @@ static hipError_t launch_product(XentProduct a, hipStream_t s) {
     a.n_tiles = (a.N + BN - 1) / BN;
     a.total = a.m_tiles * a.n_tiles * a.splits;
     a.per_split = (a.k_tiles + a.splits - 1) / a.splits;
-    SFB_LAUNCH((xent_product_kernel<WGM, WGN, MT, NT, ST, OCC, XT, YT, END, Out>), dim3(a.total), dim3(WGM * WGN * 64), lds, s, a);
+    SFB_LAUNCH((xent_product_kernel<WGM, WGN, MT, NT, ST, OCC, XT, YT, F16, END, Out>), dim3(a.total), dim3(WGM * WGN * 64), lds, s, a);
     return hipGetLastError();
 }
 
-// Tiles by the number of n (rows): m x n.
+// Tiles, m x n.
 enum XentTile { kXe256x256, kXe128x128, kXe256x64, kXe256x32 };
 static const int kXeTileM[] = {256, 128, 256, 256}, kXeTileN[] = {256, 128, 64, 32};
 
-template <bool XT, bool YT, int END, class Out>
+template <bool XT, bool YT, bool F16, int END, class Out>
 static hipError_t launch_product(const XentProduct& a, XentTile tile, hipStream_t s) {
     switch (tile) {
-        case kXe256x256: return launch_product<2, 4, 4, 2, 2, 2, XT, YT, END, Out>(a, s);
-        case kXe128x128: return launch_product<2, 2, 2, 2, 2, 2, XT, YT, END, Out>(a, s);
+        case kXe256x256: return launch_tiles<2, 4, 4, 2, 2, 2, XT, YT, F16, END, Out>(a, s);
+        case kXe128x128: return launch_tiles<2, 2, 2, 2, 2, 2, XT, YT, F16, END, Out>(a, s);
         default: break;
     }
     if constexpr (!YT) {
-        if (tile == kXe256x64) return launch_product<4, 1, 2, 2, 3, 1, XT, YT, END, Out>(a, s);
-        if (tile == kXe256x32) return launch_product<4, 1, 2, 1, 4, 1, XT, YT, END, Out>(a, s);
+        if (tile == kXe256x64) return launch_tiles<4, 1, 2, 2, 3, 1, XT, YT, F16, END, Out>(a, s);
+        if (tile == kXe256x32) return launch_tiles<4, 1, 2, 1, 4, 1, XT, YT, F16, END, Out>(a, s);
     }
     return hipErrorInvalidValue;
 }
 
-static XentTile tile_for(int64_t M, int64_t N) {
-    if (N <= 32) return kXe256x32;
-    if (N <= 64) return kXe256x64;
-    return ((M + 255) / 256) * ((N + 255) / 256) >= 192 ? kXe256x256 : kXe128x128;
+struct Tiling {
+    XentTile tile;
+    int splits;
+};
+
+// Tile and splits of k for an M x N product of `stages` stages (all pairs of terms): the fewest microseconds by what a stage takes a lone
+// workgroup, and a compute unit that is full of them.  splits <= most; each costs its plane's way to memory and back.
+static Tiling tiling_for(int64_t M, int64_t N, int64_t stages, int64_t most, bool rows_are_n) {
+    static const struct { XentTile tile; int resident; double lone_us, full_us; } kinds[] = {
+        {kXe256x256, 1, 1.70, 1.95}, {kXe128x128, 2, 0.58, 0.52}, {kXe256x64, 1, 0.60, 0.60}, {kXe256x32, 1, 0.50, 0.50}};
+    Tiling best{kXe128x128, 1};
+    double best_us = 1e300;
+    for (const auto& t : kinds) {
+        if (rows_are_n ? (t.tile == kXe256x32 && N > 32) || (t.tile == kXe256x64 && N > 64) : kXeTileN[t.tile] < 128) continue;
+        const int64_t tiles = ((M + kXeTileM[t.tile] - 1) / kXeTileM[t.tile]) * ((N + kXeTileN[t.tile] - 1) / kXeTileN[t.tile]);
+        for (int64_t s = 1; s <= most && (s == 1 || s * 4 <= stages); ++s) {
+            const int64_t n = tiles * s, deep = (n + 256 * t.resident - 1) / (256 * t.resident);
+            const double lone = t.lone_us * (double)deep, full = t.full_us * (double)((n + 255) / 256);
+            const double us = 3.0 * (double)deep + (double)((stages + s - 1) / s) * (lone > full ? lone : full) + (s > 1 ? (double)s * (double)M * (double)N * 8e-6 / 3.0 : 0.0);
+            if (us < best_us * 0.999) {
+                best_us = us;
+                best = Tiling{t.tile, (int)s};
+            }
+        }
+    }
+    return best;
 }
 
-// Pairs of terms of a product, the small ones first; `most`: the sum of their numbers (0, 1, 2) goes up to it
+// Pairs of terms of a product, the small ones first: those whose numbers (0, 1, 2) add up to `most` at most
 static int pair_list(int x_terms, int y_terms, int most, uint32_t* px, uint32_t* py) {
     int n = 0;
     *px = *py = 0;
@@ -631,240 +892,362 @@ static int pair_list(int x_terms, int y_terms, int most, uint32_t* px, uint32_t*
         }
     return n;
 }
+static int pair_count(int x_terms, int y_terms, int most) {
+    uint32_t x, y;
+    return pair_list(x_terms, y_terms, most, &x, &y);
+}
 
 namespace {
 constexpr int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+constexpr size_t kXePieceBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 30;   // of U and kept scores; of W's terms
+
+// What a call does and where it keeps it.
 struct Layout {
-    int64_t n_padded, ld_a, ld_w, piece, ld_acc;
-    int a_terms, w_terms, u_terms, k_tiles, window, splits;
-    size_t rows, label, g, lse, loss, z, count, partial, acc, a, w, u, bytes;
+    int64_t n_padded, piece, ld_k, ld_a, ld_acc;       // piece: words; ld_k: features to whole stages
+    bool f16, direct, kept;                            // fp16 terms (either operand fp32); W read as it is; scores of the one piece kept
+    int k_tiles, window;
+    int a_terms, a16_terms, w16_terms, u_terms, u16_terms;
+    int score_most, dA_most, dW_most;                  // pairs of terms
+    Tiling scores, dA, dW;
+    size_t rows, label, g, exp_g, lse, loss, z_label, count, top, exp_a, exp_w, partial, acc, a, a16, w, z, u, u16, bytes;
 };
 }  // namespace
 
-// direct: W is read as it is.  piece: words of a piece, a multiple of 256
-static Layout layout_of(const XentCall& c, bool direct, bool grads, int64_t piece) {
+static bool reads_w_directly(const XentCall& c) {
+    return c.w_bf16 && c.a_bf16 && c.D % 8 == 0 && c.D >= 64 && c.ldw % 8 == 0 && ((uintptr_t)c.W % 16) == 0 && c.ldw < (1 << 23);
+}
+
+// piece: words of a piece, a multiple of 256
+static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, int64_t piece) {
     Layout l{};
-    const int64_t n_some = c.n > 0 ? c.n : 1;
-    l.n_padded = up(n_some, 256);
-    l.k_tiles = (int)((c.D + 63) / 64);
-    l.window = direct && c.D % 64 != 0 ? 64 * l.k_tiles : 0;
-    l.ld_a = 64 * l.k_tiles + (l.window ? 64 : 0);
-    l.ld_w = 64 * l.k_tiles;
-    l.ld_acc = up(c.D, 8);
-    l.a_terms = c.a_bf16 ? 1 : 3;
-    l.w_terms = c.w_bf16 ? 1 : 3;
-    l.u_terms = grads ? (c.a_bf16 && c.w_bf16 ? 1 : 3) : 0;
+    const int64_t n = c.n > 0 ? c.n : 1, words = piece < c.J ? piece : c.J;
+    l.f16 = !(c.a_bf16 && c.w_bf16);
+    l.direct = direct;
+    l.kept = kept;
     l.piece = piece;
+    l.n_padded = up(n, 256);
+    l.k_tiles = (int)((c.D + 63) / 64);
+    l.ld_k = 64 * (int64_t)l.k_tiles;
+    l.window = direct && c.D % 64 != 0 ? (int)l.ld_k : 0;
+    l.ld_a = l.ld_k + (l.window ? 64 : 0);
+    l.ld_acc = up(c.D, 8);
+    if (l.f16) {
+        l.a16_terms = c.a_bf16 ? 1 : 2;
+        l.w16_terms = c.w_bf16 ? 1 : 2;
+        l.score_most = 1;
+        l.dA_most = c.a_bf16 ? 0 : 1;
+        l.dW_most = c.w_bf16 ? 1 : 2;
+        l.u16_terms = grads ? (c.a_bf16 ? 1 : 2) : 0;
+        l.u_terms = grads ? l.dW_most + 1 : 0;
+        l.a_terms = grads ? (c.a_bf16 ? 1 : l.dW_most + 1) : 0;
+    } else {
+        l.a_terms = 1;
+        l.u_terms = grads ? 1 : 0;
+    }
+    const int score_pairs = l.f16 ? pair_count(l.w16_terms, l.a16_terms, 1) : 1;
+    const int64_t row_tiles = (n + 63) / 64, word_tiles = (words + 63) / 64;
+    l.scores = tiling_for(words, n, (int64_t)l.k_tiles * score_pairs, kept ? 16 : 1, true);
+    if (grads) {
+        l.dA = tiling_for(c.D, n, word_tiles * (l.f16 ? pair_count(l.w16_terms, l.u16_terms, l.dA_most) : 1), 64, true);
+        if (l.dA.splits > word_tiles) l.dA.splits = (int)word_tiles;
+        l.dW = tiling_for(c.D, words, row_tiles * (l.f16 ? pair_count(l.a_terms, l.u_terms, l.dW_most) : 1), 1, false);
+    }
+    if (l.scores.splits > l.k_tiles) l.scores.splits = l.k_tiles;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t p = at;
         at += up(bytes, 256);
         return p;
     };
-    l.rows = take((size_t)n_some * 4);
+    l.rows = take((size_t)n * 4);
     l.label = take((size_t)l.n_padded * 4);
     l.g = take((size_t)l.n_padded * 4);
+    l.exp_g = take((size_t)l.n_padded * 4);
     l.lse = take((size_t)l.n_padded * 4);
     l.loss = take((size_t)l.n_padded * 4);
-    l.z = take((size_t)l.n_padded * 4);
+    l.z_label = take((size_t)l.n_padded * 4);
     l.count = take(4);
-    l.partial = take((size_t)(up(c.J, 256) / 128) * l.n_padded * 8);
-    l.a = take((size_t)l.a_terms * l.n_padded * l.ld_a * 2);
-    if (grads) {
-        // few rows leave few tiles of dA: the words are cut into splits with sums of their own
-        const XentTile t = tile_for(c.D, n_some);
-        const int64_t tiles = ((c.D + kXeTileM[t] - 1) / kXeTileM[t]) * ((n_some + kXeTileN[t] - 1) / kXeTileN[t]), most = up(piece, 64) / 64 / 8;
-        int64_t s = tiles >= 192 ? 1 : (256 + tiles - 1) / tiles;
-        if (s > most) s = most;
-        l.splits = s < 1 ? 1 : (int)s;
-        l.acc = take((size_t)l.splits * l.n_padded * l.ld_acc * 4);
-        l.u = take((size_t)l.u_terms * l.n_padded * piece * 2);
+    l.top = take(4);
+    if (l.f16) {
+        l.exp_a = take((size_t)l.n_padded * 4);
+        l.exp_w = take((size_t)piece * 4);
+        l.a16 = take((size_t)l.a16_terms * l.n_padded * l.ld_k * 2);
     }
-    if (!direct) l.w = take((size_t)l.w_terms * up(piece, 64) * l.ld_w * 2);
+    if (l.a_terms) l.a = take((size_t)l.a_terms * l.n_padded * l.ld_a * 2);
+    if (kept) l.z = take((size_t)l.scores.splits * l.n_padded * piece * 4);
+    else l.partial = take((size_t)(up(c.J, 256) / 128) * l.n_padded * 8);
+    if (grads) {
+        l.acc = take((size_t)l.dA.splits * n * l.ld_acc * 4);
+        l.u = take((size_t)l.u_terms * l.n_padded * piece * 2);
+        l.u16 = take((size_t)l.u16_terms * l.n_padded * piece * 2);
+    }
+    if (!direct) l.w = take((size_t)(l.f16 ? l.w16_terms : 1) * piece * l.ld_k * 2);
     l.bytes = at;
     return l;
 }
 
-static bool reads_w_directly(const XentCall& c) {
-    return c.w_bf16 && c.D % 8 == 0 && c.D >= 64 && c.ldw % 8 == 0 && ((uintptr_t)c.W % 16) == 0 && c.ldw < (1 << 23);
+// Whether a call keeps its scores: they fit, and forming them again (or leaving most compute units idle) would take longer than their
+// way to memory and back.  A score costs 2 D flops a pair of terms again, at about 1 PFLOP/s, or some 12 bytes at 4 TB/s.
+static bool keeps_scores(const XentCall& c, bool forward, bool grads) {
+    const int64_t n = c.n > 0 ? c.n : 1, whole = up(c.J, 256);
+    if ((size_t)up(n, 256) * whole * 4 * 2 > kXePieceBytes) return false;
+    const int pairs = c.a_bf16 && c.w_bf16 ? 1 : c.a_bf16 || c.w_bf16 ? 2 : 3;
+    const int64_t tiles = ((c.J + 127) / 128) * ((n + 127) / 128);
+    return n > 64 && ((forward && grads && c.D * pairs >= 1500) || (tiles < 200 && c.D * pairs >= 1500));
+}
+
+// The layout that a call on c's sizes takes within `bytes`; .bytes > bytes: there is none
+static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads, size_t bytes) {
+    const int64_t whole = up(c.J, 256) / 256;
+    if (keeps_scores(c, forward, grads)) {
+        const Layout l = layout_of(c, direct, grads, true, whole * 256);
+        if (l.bytes <= bytes) return l;
+    }
+    if (!grads && direct) return layout_of(c, true, false, false, whole * 256);
+    // the most words whose U and whose W's terms stay within their bounds, and the whole within `bytes`
+    const Layout one = layout_of(c, direct, grads, false, 256);
+    const size_t u_bytes = (size_t)(one.u_terms + one.u16_terms) * one.n_padded * 512, w_bytes = direct ? 0 : (size_t)(one.f16 ? one.w16_terms : 1) * one.ld_k * 512;
+    int64_t lo = 1, hi = whole < (1 << 14) ? whole : (1 << 14);          // 32-bit offsets inside a tile: 2^22 words at most
+    if (u_bytes > 0 && hi > (int64_t)(kXePieceBytes / u_bytes)) hi = (int64_t)(kXePieceBytes / u_bytes);
+    if (w_bytes > 0 && hi > (int64_t)(kXeWordBytes / w_bytes)) hi = (int64_t)(kXeWordBytes / w_bytes);
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) / 2;
+        if (layout_of(c, direct, grads, false, mid * 256).bytes <= bytes) lo = mid; else hi = mid - 1;
+    }
+    const int64_t pieces = (whole + lo - 1) / lo;                        // evened out
+    const Layout l = layout_of(c, direct, grads, false, (whole + pieces - 1) / pieces * 256);
+    return l.bytes <= bytes ? l : layout_of(c, direct, grads, false, lo * 256);
 }
 
 size_t xent_workspace(const XentCall& c, bool grads, bool least) {
-    const int64_t whole = up(c.J, 256);
-    if (least) return layout_of(c, false, grads, 256).bytes > layout_of(c, true, grads, 256).bytes ? layout_of(c, false, grads, 256).bytes
-                                                                                                  : layout_of(c, true, grads, 256).bytes;
-    // pieces of 256 MB of U and W together
-    const bool direct = c.w_bf16 && c.D % 8 == 0 && c.D >= 64;
-    const Layout one = layout_of(c, direct, grads, 256), two = layout_of(c, direct, grads, 512);
-    int64_t pieces = (int64_t)(((size_t)256 << 20) / (two.bytes - one.bytes + 1));
-    if (pieces < 4) pieces = 4;
-    const size_t b = layout_of(c, direct, grads, pieces * 256 < whole ? pieces * 256 : whole).bytes, m = xent_workspace(c, grads, true);
-    return b > m ? b : m;
-}
-
-// The largest piece that the workspace holds, evened out over the pieces; 0: none.
-static int64_t piece_for(const XentCall& c, bool direct, bool grads, size_t bytes) {
-    const int64_t whole = up(c.J, 256) / 256;
-    if (!grads && direct) return layout_of(c, true, false, 256).bytes <= bytes ? whole * 256 : 0;
-    int64_t lo = 0, hi = whole < (1 << 14) ? whole : (1 << 14);          // 32-bit offsets inside a tile: 2^22 words at most
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) / 2;
-        if (layout_of(c, direct, grads, mid * 256).bytes <= bytes) lo = mid; else hi = mid - 1;
+    const bool direct = c.w_bf16 && c.a_bf16 && c.D % 8 == 0 && c.D >= 64;
+    size_t m = 0;
+    // fewer rows can take more splits: the least is what the smallest piece takes at the most splits
+    for (int d = 0; d < 2; ++d) {
+        if (d && !direct) break;
+        Layout l = layout_of(c, d != 0, grads, false, 256);
+        size_t b = l.bytes;
+        if (grads) b += (size_t)(4 - l.dA.splits > 0 ? 4 - l.dA.splits : 0) * (size_t)(c.n > 0 ? c.n : 1) * l.ld_acc * 4;
+        if (b > m) m = b;
     }
-    if (lo == 0) return 0;
-    const int64_t pieces = (whole + lo - 1) / lo;
-    return (whole + pieces - 1) / pieces * 256;
+    if (least) return m;
+    for (int f = 0; f < 2; ++f) {
+        const size_t b = plan_call(c, direct, f != 0, grads, ~(size_t)0).bytes;
+        if (b > m) m = b;
+    }
+    return m;
 }
 
 hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t s) {
     const bool direct = reads_w_directly(c);
-    const int64_t piece = piece_for(c, direct, grads, c.ws_bytes);
-    if (piece == 0) return hipErrorInvalidValue;
-    const Layout l = layout_of(c, direct, grads, piece);
+    const Layout l = plan_call(c, direct, forward, grads, c.ws_bytes);
+    if (l.bytes > c.ws_bytes) return hipErrorInvalidValue;
     char* const ws = (char*)c.ws;
     int* const rows = (int*)(ws + l.rows);
     int* const label = (int*)(ws + l.label);
     int* const count = (int*)(ws + l.count);
+    int* const top = (int*)(ws + l.top);
     float* const g = (float*)(ws + l.g);
+    int* const exp_g = (int*)(ws + l.exp_g);
     float* const lse = (float*)(ws + l.lse);
     float* const loss = (float*)(ws + l.loss);
     bf16_t* const A = (bf16_t*)(ws + l.a);
+    bf16_t* const A16 = (bf16_t*)(ws + l.a16);
     bf16_t* const Wp = (bf16_t*)(ws + l.w);
-    const int64_t a_plane = l.n_padded * l.ld_a;
+    int* const exp_a = (int*)(ws + l.exp_a);
+    int* const exp_w = (int*)(ws + l.exp_w);
+    const int64_t a_plane = l.n_padded * l.ld_a, a16_plane = l.n_padded * l.ld_k, w_plane = l.piece * l.ld_k;
     const int64_t n_some = c.n > 0 ? c.n : 1;                            // an empty batch: nothing takes part, dW is 0
+    const int* const none = nullptr;
+    float* const nowhere = nullptr;
     hipError_t e;
 
-    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, c.y, (int)c.n, (int)c.J, c.weight, c.scale, c.mean, rows, label, g, count);
-    const uint32_t pack_grid = (uint32_t)((l.n_padded * (l.ld_a / 8) + 255) / 256);
-    float* const loss0 = forward ? c.loss : nullptr;
-    float* const lse0 = forward ? c.lse : nullptr;
-    if (c.a_bf16)
-        hipLaunchKernelGGL(xent_pack_kernel<bf16_t>, dim3(pack_grid), dim3(256), 0, s, (const bf16_t*)c.a, c.lda, (int)c.D, (const int*)rows, (const int*)count,
-                           (int)c.n, (int)l.n_padded, A, l.ld_a, a_plane, l.a_terms, l.window, (bf16_t*)(grads ? c.dA : nullptr), c.ldda, loss0, lse0);
-    else
-        hipLaunchKernelGGL(xent_pack_kernel<float>, dim3(pack_grid), dim3(256), 0, s, (const float*)c.a, c.lda, (int)c.D, (const int*)rows, (const int*)count,
-                           (int)c.n, (int)l.n_padded, A, l.ld_a, a_plane, l.a_terms, l.window, (float*)(grads ? c.dA : nullptr), c.ldda, loss0, lse0);
+    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, c.y, (int)c.n, (int)c.J, c.weight, c.scale, c.mean, rows, label, g, exp_g, count);
+    {
+        // (one term at least: what takes no part gets its zeros here)
+        const int64_t ld = l.a_terms ? l.ld_a : l.ld_k;
+        const uint32_t grid = (uint32_t)((l.n_padded * (ld / 8) + 255) / 256);
+        float* const loss0 = forward ? c.loss : nullptr;
+        float* const lse0 = forward ? c.lse : nullptr;
+        void* const dA0 = grads ? c.dA : nullptr;
+        if (c.a_bf16)
+            hipLaunchKernelGGL(xent_pack_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const bf16_t*)c.a, c.lda, (int)c.D, (const int*)rows, (const int*)count,
+                               (int)c.n, (int)l.n_padded, A, ld, a_plane, l.a_terms, l.window, (bf16_t*)dA0, c.ldda, loss0, lse0);
+        else
+            hipLaunchKernelGGL(xent_pack_kernel<float>, dim3(grid), dim3(256), 0, s, (const float*)c.a, c.lda, (int)c.D, (const int*)rows, (const int*)count,
+                               (int)c.n, (int)l.n_padded, A, ld, a_plane, l.a_terms, l.window, (float*)dA0, c.ldda, loss0, lse0);
+    }
+    if (l.f16) {
+        if (c.a_bf16)
+            hipLaunchKernelGGL(xent_pack16_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, (const bf16_t*)c.a, c.lda, (int)c.D, (const int*)rows,
+                               (const int*)count, (int)c.n, A16, l.ld_k, a16_plane, l.a16_terms, exp_a);
+        else
+            hipLaunchKernelGGL(xent_pack16_kernel<float>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, (const float*)c.a, c.lda, (int)c.D, (const int*)rows,
+                               (const int*)count, (int)c.n, A16, l.ld_k, a16_plane, l.a16_terms, exp_a);
+    }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
 
-    // X = W's rows first .. first + words - 1 in terms
+    // W's rows first .. first + n - 1 as an operand
     struct Words { const bf16_t* p; int64_t ld, plane; int rows; };
+    int64_t there = -1;                                                  // the piece whose terms are in the workspace
     auto words = [&](int64_t first, int64_t n, Words* w) -> hipError_t {
         if (direct) {
             *w = Words{(const bf16_t*)c.W + first * c.ldw, c.ldw, 0, (int)n};
             return hipSuccess;
         }
-        const int64_t padded = up(n, 64), plane = up(piece, 64) * l.ld_w;
-        const uint32_t grid = (uint32_t)((padded * (l.ld_w / 8) + 255) / 256);
+        const int64_t padded = up(n, 64);
+        *w = Words{Wp, l.ld_k, w_plane, (int)padded};
+        if (there == first) return hipSuccess;
+        there = first;
+        if (!l.f16) {
+            const uint32_t grid = (uint32_t)((padded * (l.ld_k / 8) + 255) / 256);
+            hipLaunchKernelGGL(xent_pack_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D, none, none, (int)n,
+                               (int)padded, Wp, l.ld_k, w_plane, 1, 0, (bf16_t*)nullptr, (int64_t)0, nowhere, nowhere);
+            return hipGetLastError();
+        }
         if (c.w_bf16)
-            hipLaunchKernelGGL(xent_pack_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D, (const int*)nullptr,
-                               (const int*)nullptr, (int)n, (int)padded, Wp, l.ld_w, plane, 1, 0, (bf16_t*)nullptr, (int64_t)0, (float*)nullptr, (float*)nullptr);
+            hipLaunchKernelGGL(xent_pack16_kernel<bf16_t>, dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D, none,
+                               none, (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
         else
-            hipLaunchKernelGGL(xent_pack_kernel<float>, dim3(grid), dim3(256), 0, s, (const float*)c.W + first * c.ldw, c.ldw, (int)c.D, (const int*)nullptr,
-                               (const int*)nullptr, (int)n, (int)padded, Wp, l.ld_w, plane, 3, 0, (float*)nullptr, (int64_t)0, (float*)nullptr, (float*)nullptr);
-        *w = Words{Wp, l.ld_w, plane, (int)padded};
+            hipLaunchKernelGGL(xent_pack16_kernel<float>, dim3((uint32_t)padded), dim3(256), 0, s, (const float*)c.W + first * c.ldw, c.ldw, (int)c.D, none, none,
+                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
+        if (grads) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)exp_w, (int)n, top);
         return hipGetLastError();
     };
     XentProduct scores{};
-    scores.y = A; scores.ldy = l.ld_a; scores.y_plane = a_plane; scores.y_rows = (int)l.n_padded;
+    scores.y = l.f16 ? A16 : A; scores.ldy = l.f16 ? l.ld_k : l.ld_a; scores.y_plane = l.f16 ? a16_plane : a_plane; scores.y_rows = (int)l.n_padded;
     scores.N = (int)n_some; scores.k_tiles = l.k_tiles;
     scores.last_x = l.window ? (int)c.D - 64 : 64 * (l.k_tiles - 1);
     scores.last_y = l.window ? l.window : 64 * (l.k_tiles - 1);
-    scores.pairs = pair_list(l.w_terms, l.a_terms, 2, &scores.pair_x, &scores.pair_y);
+    scores.pairs = l.f16 ? pair_list(l.w16_terms, l.a16_terms, l.score_most, &scores.pair_x, &scores.pair_y) : 1;
+    scores.exp_m = exp_w; scores.exp_n = exp_a;
     scores.splits = 1;
     scores.count = count; scores.n_is_rows = true;
     scores.label = label; scores.ld_rows = (int)l.n_padded;
-    scores.z_label = (float*)(ws + l.z);
+    scores.z_label = (float*)(ws + l.z_label);
     scores.lse = lse; scores.g = g;
     auto scores_of = [&](int64_t first, int64_t n, const Words& w) {
         scores.x = w.p; scores.ldx = w.ld; scores.x_plane = w.plane; scores.x_rows = w.rows;
         scores.M = (int)n; scores.first_word = (int)first;
     };
+    bf16_t* const U = (bf16_t*)(ws + l.u);
+    bf16_t* const U16 = (bf16_t*)(ws + l.u16);
+    const int64_t u_plane = l.n_padded * l.piece, acc_plane = n_some * l.ld_acc;
 
-    if (forward) {
-        int tiles = 0;
-        for (int64_t first = 0; first < c.J; first += piece) {
-            const int64_t n = c.J - first < piece ? c.J - first : piece;
-            Words w;
-            e = words(first, n, &w);
-            if (e != hipSuccess) return e;
-            scores_of(first, n, w);
-            const XentTile t = tile_for(n, n_some);
-            scores.partial = (float2*)(ws + l.partial) + (int64_t)tiles * l.n_padded;
-            e = launch_product<false, false, kXeStats, float>(scores, t, s);
-            if (e != hipSuccess) return e;
-            tiles += (int)((n + kXeTileM[t] - 1) / kXeTileM[t]);
-        }
-        hipLaunchKernelGGL(xent_loss_kernel, dim3((uint32_t)((n_some + 3) / 4)), dim3(256), 0, s, (const float2*)(ws + l.partial), tiles, (int)l.n_padded,
-                           (const int*)rows, (const int*)count, (const float*)(ws + l.z), c.loss, c.lse, lse, loss);
-        if (c.total)
-            hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, c.total);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    } else {
+    if (!forward) {
         hipLaunchKernelGGL(xent_gather_kernel, dim3((uint32_t)((n_some + 255) / 256)), dim3(256), 0, s, (const float*)c.lse, (const int*)rows, (const int*)count, lse);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!grads) return hipSuccess;
+    if (l.kept) {
+        Words w;
+        e = words(0, c.J, &w);
+        if (e != hipSuccess) return e;
+        XentProduct p = scores;
+        p.x = w.p; p.ldx = w.ld; p.x_plane = w.plane; p.x_rows = w.rows;
+        p.M = (int)c.J;
+        p.splits = l.scores.splits;
+        p.out = ws + l.z; p.ldo = l.piece; p.out_plane = l.n_padded * l.piece; p.wide = true;
+        e = l.f16 ? launch_product<false, false, true, kXeStore, float>(p, l.scores.tile, s) : launch_product<false, false, false, kXeStore, float>(p, l.scores.tile, s);
+        if (e != hipSuccess) return e;
+        XentRows r{};
+        r.z = (const float*)(ws + l.z); r.ldz = l.piece; r.z_plane = p.out_plane; r.splits = l.scores.splits;
+        r.words = (int)c.J; r.columns = grads ? (int)l.piece : 0;
+        r.rows = rows; r.label = label; r.count = count; r.g = g;
+        r.loss = forward ? c.loss : nullptr; r.lse = forward ? c.lse : nullptr; r.loss_packed = loss; r.lse_packed = lse;
+        r.u = U; r.u16 = U16; r.ldu = l.piece; r.u_plane = u_plane; r.u_terms = l.u_terms; r.u16_terms = l.u16_terms;
+        r.exp_m = exp_w; r.exp_g = exp_g; r.exp_words = top;
+        r.given = !forward;
+        hipLaunchKernelGGL(xent_row_kernel, dim3((uint32_t)up(n_some, 64)), dim3(kXeRowThreads), 0, s, r);
+    } else if (forward) {
+        int tiles = 0;
+        for (int64_t first = 0; first < c.J; first += l.piece) {
+            const int64_t n = c.J - first < l.piece ? c.J - first : l.piece;
+            Words w;
+            e = words(first, n, &w);
+            if (e != hipSuccess) return e;
+            scores_of(first, n, w);
+            scores.partial = (float2*)(ws + l.partial) + (int64_t)tiles * l.n_padded;
+            e = l.f16 ? launch_product<false, false, true, kXeStats, float>(scores, l.scores.tile, s)
+                      : launch_product<false, false, false, kXeStats, float>(scores, l.scores.tile, s);
+            if (e != hipSuccess) return e;
+            tiles += (int)((n + kXeTileM[l.scores.tile] - 1) / kXeTileM[l.scores.tile]);
+        }
+        hipLaunchKernelGGL(xent_loss_kernel, dim3((uint32_t)((n_some + 3) / 4)), dim3(256), 0, s, (const float2*)(ws + l.partial), tiles, (int)l.n_padded,
+                           (const int*)rows, (const int*)count, (const float*)(ws + l.z_label), c.loss, c.lse, lse, loss);
+    }
+    if (forward && c.total)
+        hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, c.total);
+    e = hipGetLastError();
+    if (e != hipSuccess || !grads) return e;
 
-    bf16_t* const U = (bf16_t*)(ws + l.u);
-    const int64_t u_plane = l.n_padded * piece, acc_plane = l.n_padded * l.ld_acc;
-    for (int64_t first = 0; first < c.J; first += piece) {
-        const int64_t n = c.J - first < piece ? c.J - first : piece;
+    // from the last piece back: its terms of W are still there
+    const int64_t pieces = (c.J + l.piece - 1) / l.piece;
+    for (int64_t i = pieces - 1; i >= 0; --i) {
+        const int64_t first = i * l.piece, n = c.J - first < l.piece ? c.J - first : l.piece;
         Words w;
         e = words(first, n, &w);
         if (e != hipSuccess) return e;
-        scores_of(first, n, w);
-        scores.u = U; scores.ldu = piece; scores.u_plane = u_plane; scores.u_terms = l.u_terms;
-        e = launch_product<false, false, kXeU, float>(scores, tile_for(n, n_some), s);
-        if (e != hipSuccess) return e;
+        if (!l.kept) {
+            scores_of(first, n, w);
+            scores.u = U; scores.u16 = U16; scores.ldu = l.piece; scores.u_plane = u_plane; scores.u_terms = l.u_terms; scores.u16_terms = l.u16_terms;
+            scores.exp_g = exp_g; scores.exp_words = top;
+            e = l.f16 ? launch_product<false, false, true, kXeU, float>(scores, l.scores.tile, s) : launch_product<false, false, false, kXeU, float>(scores, l.scores.tile, s);
+            if (e != hipSuccess) return e;
+        }
         if (c.dA) {
             XentProduct p{};
-            p.x = w.p; p.ldx = w.ld; p.x_plane = w.plane; p.x_rows = w.rows; p.x_cols = direct ? (int)c.D : (int)l.ld_w;
-            p.y = U; p.ldy = piece; p.y_plane = u_plane; p.y_rows = (int)l.n_padded;
+            p.x = w.p; p.ldx = w.ld; p.x_plane = w.plane; p.x_rows = w.rows; p.x_cols = direct ? (int)c.D : (int)l.ld_k;
+            p.y = l.f16 ? U16 : U; p.ldy = l.piece; p.y_plane = u_plane; p.y_rows = (int)l.n_padded;
             p.M = (int)c.D; p.N = (int)n_some;
             p.k_tiles = (int)((n + 63) / 64); p.last_y = 64 * (p.k_tiles - 1);
-            // a bf16 dA is rounded to 2^-9 itself: the second terms' own products are beside it
-            p.pairs = pair_list(l.w_terms, l.u_terms, c.a_bf16 ? (l.w_terms > 1 ? 1 : 0) : 2, &p.pair_x, &p.pair_y);
-            p.splits = l.splits;
+            p.pairs = l.f16 ? pair_list(l.w16_terms, l.u16_terms, l.dA_most, &p.pair_x, &p.pair_y) : 1;
+            p.exp_n = exp_g; p.exp_top = top;
+            p.splits = l.dA.splits;
             p.count = count; p.n_is_rows = true;
-            p.out = ws + l.acc; p.ldo = l.ld_acc; p.out_plane = acc_plane; p.wide = true;
-            p.add = first > 0 ? (const float*)(ws + l.acc) : nullptr; p.ld_add = l.ld_acc;
-            e = launch_product<true, false, kXeStore, float>(p, tile_for(c.D, n_some), s);
+            if (l.dA.splits == 1 && i == 0) {                            // the last sum goes straight to its row
+                p.out = c.dA; p.ldo = c.ldda; p.row_map = rows;
+                p.wide = c.ldda % 8 == 0 && ((uintptr_t)c.dA % 16) == 0;
+            } else {
+                p.out = ws + l.acc; p.ldo = l.ld_acc; p.out_plane = acc_plane; p.wide = true;
+            }
+            p.add = i < pieces - 1 ? (const float*)(ws + l.acc) : nullptr; p.ld_add = l.ld_acc;
+            if (p.row_map && c.a_bf16)
+                e = l.f16 ? launch_product<true, false, true, kXeStore, bf16_t>(p, l.dA.tile, s) : launch_product<true, false, false, kXeStore, bf16_t>(p, l.dA.tile, s);
+            else
+                e = l.f16 ? launch_product<true, false, true, kXeStore, float>(p, l.dA.tile, s) : launch_product<true, false, false, kXeStore, float>(p, l.dA.tile, s);
             if (e != hipSuccess) return e;
         }
         if (c.dW) {
             XentProduct p{};
-            p.x = A; p.ldx = l.ld_a; p.x_plane = a_plane; p.x_rows = (int)l.n_padded; p.x_cols = (int)l.ld_w;
-            p.y = U; p.ldy = piece; p.y_plane = u_plane; p.y_rows = (int)l.n_padded; p.y_cols = (int)piece;
+            p.x = A; p.ldx = l.ld_a; p.x_plane = a_plane; p.x_rows = (int)l.n_padded; p.x_cols = (int)l.ld_k;
+            p.y = U; p.ldy = l.piece; p.y_plane = u_plane; p.y_rows = (int)l.n_padded; p.y_cols = (int)l.piece;
             p.M = (int)c.D; p.N = (int)n;
             p.k_tiles = (int)((n_some + 63) / 64);
-            p.pairs = pair_list(l.a_terms, l.u_terms, c.w_bf16 ? (l.a_terms > 1 ? 1 : 0) : 2, &p.pair_x, &p.pair_y);
+            p.pairs = l.f16 ? pair_list(l.a_terms, l.u_terms, l.dW_most, &p.pair_x, &p.pair_y) : 1;
             p.splits = 1;
             p.count = count; p.k_is_rows = true;
             p.ldo = c.lddw;
             if (c.w_bf16) {
                 p.out = (bf16_t*)c.dW + first * c.lddw;
                 p.wide = c.lddw % 8 == 0 && ((uintptr_t)c.dW % 16) == 0;
-                const XentTile t = ((c.D + 255) / 256) * ((n + 255) / 256) >= 192 ? kXe256x256 : kXe128x128;
-                e = launch_product<true, true, kXeStore, bf16_t>(p, t, s);
+                e = launch_product<true, true, false, kXeStore, bf16_t>(p, l.dW.tile, s);
             } else {
                 p.out = (float*)c.dW + first * c.lddw;
                 p.wide = c.lddw % 4 == 0 && ((uintptr_t)c.dW % 16) == 0;
-                const XentTile t = ((c.D + 255) / 256) * ((n + 255) / 256) >= 192 ? kXe256x256 : kXe128x128;
-                e = launch_product<true, true, kXeStore, float>(p, t, s);
+                e = launch_product<true, true, false, kXeStore, float>(p, l.dW.tile, s);
             }
             if (e != hipSuccess) return e;
         }
     }
-    if (c.dA) {
+    if (c.dA && l.dA.splits > 1) {
         const uint32_t grid = (uint32_t)((n_some * ((c.D + 3) / 4) + 255) / 256);
         if (c.a_bf16)
-            hipLaunchKernelGGL(xent_rows_out_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const float*)(ws + l.acc), l.ld_acc, acc_plane, l.splits,
+            hipLaunchKernelGGL(xent_rows_out_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const float*)(ws + l.acc), l.ld_acc, acc_plane, l.dA.splits,
                                (const int*)rows, (const int*)count, (int)c.D, (bf16_t*)c.dA, c.ldda);
         else
-            hipLaunchKernelGGL(xent_rows_out_kernel<float>, dim3(grid), dim3(256), 0, s, (const float*)(ws + l.acc), l.ld_acc, acc_plane, l.splits,
+            hipLaunchKernelGGL(xent_rows_out_kernel<float>, dim3(grid), dim3(256), 0, s, (const float*)(ws + l.acc), l.ld_acc, acc_plane, l.dA.splits,
                                (const int*)rows, (const int*)count, (int)c.D, (float*)c.dA, c.ldda);
         e = hipGetLastError();
     }

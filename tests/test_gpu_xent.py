@@ -82,8 +82,11 @@ def _check(got, want, dtype, w_dtype, D, what):
         allow = 2 * HALF[t] * w.abs() + 2.0 ** -22 * 8 * want[k + "_abs"] + 2 * ez * (want["p_" + k] + (want["l_dA"] if k == "dA" else want["dW_abs"]))
         if both:
             allow = allow + 6 * 2 * HALF["bf16"] * want[k + "_sq"]
-        elif t == "bf16":
+        elif t == "bf16" and k == "dW":
             allow = allow + 6 * 2.0 ** -17 * want[k + "_abs"]         # second terms' own products left out
+        elif t == "bf16":
+            # one fp16 term of U and of W, 11 bits each: at most half a step off, 2^-11 of a value, so a product 2^-10 (1 + 2^-12)
+            allow = allow + (2.0 ** -10 + 2.0 ** -22) * want[k + "_abs"]
         allow = allow + 1e-30
         worst = float(((x - w).abs() / allow).max())
         assert worst <= 1.0, f"{what}: {k} {worst:.3g} x the allowance"
@@ -139,6 +142,32 @@ def test_small_and_odd_sizes(n, J, D, dtype, w_dtype):
 @pytest.mark.parametrize("dtype,w_dtype", PAIRS)
 def test_large_tiles(dtype, w_dtype):
     _run(1000, 12345, 520, dtype, w_dtype, seed=3, padded=0.1)
+
+
+@pytest.mark.parametrize("dtype,w_dtype", PAIRS)
+@pytest.mark.parametrize("two", [False, True])
+def test_long_features(two, dtype, w_dtype):
+    """Few tiles and a long contraction: the scores in slices of D."""
+    _run(130, 1001, 1607, dtype, w_dtype, seed=30, padded=0.1, two=two)
+    _run(65, 300, 4096, dtype, w_dtype, seed=31, weighted=True, two=two, spread=4.0)
+
+
+@pytest.mark.parametrize("dtype,w_dtype", PAIRS)
+def test_rows_and_words_of_very_different_size(dtype, w_dtype):
+    """Rows of a and of W 2^-20 to 2^20 of their neighbours', scores of ordinary size all the same."""
+    import paper_1511_08486_amd as sfb
+    n, J, D = 96, 520, 640
+    W, a, y = _inputs(n, J, D, dtype, w_dtype, 33)
+    W[::3] *= 2.0 ** -20
+    W[1::3, :8] *= 2.0 ** 10
+    a[::2, :8] *= 2.0 ** -12
+    W = torch.where(torch.rand(J, 1, generator=torch.Generator().manual_seed(5)).to(DEV) < 0.1, torch.zeros_like(W), W)
+    weight = (2.0 ** torch.randint(-20, 20, (n,), generator=torch.Generator().manual_seed(6)).float()).to(DEV)
+    o = dict(loss=torch.empty(n, device=DEV), lse=torch.empty(n, device=DEV), total=torch.empty(1, device=DEV), dA=torch.empty_like(a), dW=torch.empty_like(W))
+    head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype=w_dtype)
+    head.loss_and_gradients(W, a, y, **o, weight=weight)
+    head.sync()
+    _check(o, _formula(W, a, y, weight), dtype, w_dtype, D, f"{dtype}/{w_dtype}")
 
 
 def test_many_rows():
