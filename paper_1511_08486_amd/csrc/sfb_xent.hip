@@ -77,12 +77,12 @@ __device__ __forceinline__ float xe_exp(float x) {
 }
 
 // How one operand goes to LDS and comes from there.  ROWS: of m (n) in the tile.  Not TR: LDS rows of 64 k, 16-byte piece p of row r at
-// p ^ (r & 7).  TR: LDS rows of ROWS m, 32-byte piece p of k-row r at p ^ turn(r), so that the four rows of a transposing read, and its
+// p ^ (r & 7) ^ (r >> 3 & 1): sixteen consecutive rows on sixteen different bank groups (without the last bit half of all reads waited).  TR: LDS rows of ROWS m, 32-byte piece p of k-row r at p ^ turn(r), so that the four rows of a transposing read, and its
 // neighbour's sixteen columns, fall on different banks.
 template <bool TR, int ROWS, int WAVES, int TILES>
 struct XentSide {
     static constexpr int LOADS = ROWS / 8 / WAVES, BYTES = ROWS * 128;
-    static_assert(LOADS * 8 * WAVES == ROWS, "whole accesses");
+    static_assert(LOADS * 8 * WAVES == ROWS && WAVES % 2 == 0, "whole accesses");
     uint32_t off[LOADS];
     int at[TR ? TILES : 4];
     __device__ __forceinline__ static int turn(int r) { return ROWS >= 128 ? 2 * (r & 3) : r & 3; }
@@ -92,7 +92,7 @@ struct XentSide {
         for (int i = 0; i < LOADS; ++i) {
             if constexpr (!TR) {
                 const int r = min(row0 + (i * WAVES + wave) * 8 + (lane >> 3), rows - 1) - row0;
-                off[i] = (uint32_t)r * (uint32_t)ld * 2u + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7)) * 16);
+                off[i] = (uint32_t)r * (uint32_t)ld * 2u + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7) ^ (wave & 1)) * 16);
             } else {
                 constexpr int PER = ROWS / 8;
                 const int q = (i * WAVES + wave) * 64 + lane, r = q / PER, p = q % PER;
@@ -106,7 +106,7 @@ struct XentSide {
         const int l32 = lane & 31, half = lane >> 5;
         if constexpr (!TR) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) at[s] = (first + l32) * 128 + (((2 * s + half) ^ (l32 & 7)) << 4);
+            for (int s = 0; s < 4; ++s) at[s] = (first + l32) * 128 + (((2 * s + half) ^ (l32 & 7) ^ ((l32 >> 3) & 1)) << 4);
         } else {
             // sixteen lanes read four k of sixteen columns and are handed a column each; the next sixteen the other columns, the next k eight on
             const int g = lane >> 4, l16 = lane & 15, k = 8 * (g >> 1) + (l16 >> 2);
@@ -502,21 +502,43 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
 // ---------------------------------------------------------------------------------------------------------------
 // What stands around the products
 
-// One workgroup: the rows that take part, in order, then the others; label and factor of each of the former.
-__global__ __launch_bounds__(1024) void xent_rows_kernel(const int32_t* __restrict__ y, int n, int J, const float* __restrict__ weight, float scale,
-                                                         int mean, int* __restrict__ rows, int* __restrict__ label, float* __restrict__ g,
-                                                         int* __restrict__ exp_g, int* __restrict__ count) {
-    __shared__ int before[16], total;
+constexpr int kXeFewRows = 1024;   // up to so many every workgroup that packs finds the rows that take part by itself
+
+struct XentPack {
+    const void* a;
+    int64_t lda;
+    int n, J, D, n_padded;
+    const int32_t* y;
+    const float* weight;
+    float scale;
+    int mean;
+    int *rows, *label, *exp_g, *count;       // what the later kernels read
+    float* g;
+    bf16_t *to, *to16;                       // bf16 and fp16 terms, [terms][n_padded][ld]
+    int64_t ld, plane, ld16, plane16;
+    int terms, terms16, window;
+    int* exps;
+    void* zero;                              // dA, loss, lse of the rows that take no part; or nullptr
+    int64_t ld_zero;
+    float *loss, *lse;
+};
+
+// The rows that take part in front, in order, then the others; label, factor and its exponent of each of the former.  All threads of a
+// workgroup of 64 `waves`; what is found of row `mine` of the packed order is returned (source row, or -1 behind n), and the count.
+__device__ __forceinline__ int xe_find_rows(const XentPack& p, int mine, bool write, int waves, int* found_count) {
+    __shared__ int before[16], total, source;
     int taken = 0;                                                       // so far, the same in every thread
-    for (int base = 0; base < n; base += 1024) {
-        const int i = base + (int)threadIdx.x, lab = i < n ? y[i] : -1;
-        const bool real = lab >= 0 && lab < J;
+    if (threadIdx.x == 0) source = -1;
+    const int threads = 64 * waves;
+    for (int base = 0; base < p.n; base += threads) {
+        const int i = base + (int)threadIdx.x, lab = i < p.n ? p.y[i] : -1;
+        const bool real = lab >= 0 && lab < p.J;
         const uint64_t votes = __ballot(real);
         if ((threadIdx.x & 63) == 0) before[threadIdx.x >> 6] = __popcll(votes);
         __syncthreads();
         if (threadIdx.x == 0) {
             int s = taken;
-            for (int w = 0; w < 16; ++w) {
+            for (int w = 0; w < waves; ++w) {
                 const int c = before[w];
                 before[w] = s;
                 s += c;
@@ -525,104 +547,136 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(const int32_t* __restri
         }
         __syncthreads();
         const int k = before[threadIdx.x >> 6] + __popcll(votes & ((1ull << (threadIdx.x & 63)) - 1ull));
-        if (real) {
-            rows[k] = i;
-            label[k] = lab;
-            g[k] = scale * (weight ? weight[i] : 1.f);
-        } else if (i < n) {
-            rows[n - 1 - (i - k)] = i;                                   // i - k rows before this one take no part
+        const int at = real ? k : p.n - 1 - (i - k);                     // i - k rows before this one take no part
+        if (i < p.n) {
+            if (at == mine) source = i;
+            if (write) {
+                p.rows[at] = i;
+                if (real) {
+                    p.label[k] = lab;
+                    p.g[k] = p.scale * (p.weight ? p.weight[i] : 1.f);
+                }
+            }
         }
         taken = total;
         __syncthreads();
     }
-    for (int k = threadIdx.x; k < taken; k += 1024) {                    // (written before the last barrier)
-        const float x = mean ? g[k] / (float)taken : g[k];
-        g[k] = x;
-        exp_g[k] = (int)(__float_as_uint(x) >> 23 & 255u) - 127 - 14;    // |u| <= |g| is below 2^15 of it
-    }
-    if (threadIdx.x == 0) *count = taken;
-}
-
-// Rows of `src` in bf16 terms, k padded with zeros to whole stages.  rows: row of src for every packed row (the first *count of them; a row
-// behind those takes its results' zeros here), or nullptr: rows 0 .. n - 1.  window: one stage more that repeats the last 64
-// columns of src, with zeros where they are in the stage before: it meets W's last 64 columns where W is read as it is.
-template <class T>
-__global__ __launch_bounds__(256) void xent_pack_kernel(const T* __restrict__ src, int64_t ld, int D, const int* __restrict__ rows,
-                                                        const int* __restrict__ count, int n, int n_padded, bf16_t* __restrict__ dst, int64_t ldd,
-                                                        int64_t plane, int terms, int window, T* __restrict__ zero, int64_t ld_zero,
-                                                        float* __restrict__ loss, float* __restrict__ lse) {
-    const int per = (int)(ldd / 8);
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int k = (int)(c / per), p = (int)(c % per);
-    if (k >= n_padded) return;
-    const int real = rows ? min(*count, n) : n;
-    if (rows && k >= real && k < n) {
-        const int i = rows[k];
-        if (zero)
-            for (int d = p * 8; d < min(D, p * 8 + 8); ++d) zero[(int64_t)i * ld_zero + d] = T(0);
-        if (p == 0 && loss) loss[i] = 0.f;
-        if (p == 0 && lse) lse[i] = 0.f;
-    }
-    float x[8];
-    const int at = window && p * 8 >= window ? D - 64 + (p * 8 - window) : p * 8;
-    const int least = window && p * 8 >= window ? window - 64 : 0;
-    const T* row = src + (int64_t)(rows && k < real ? rows[k] : min(k, n - 1)) * ld;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int d = at + e;
-        const bool in = k < real && d < D && d >= least;
-        if constexpr (sizeof(T) == 4) x[e] = in ? row[d] : 0.f;
-        else x[e] = in ? bf16_to_f32(row[d]) : 0.f;
-    }
-    for (int t = 0; t < terms; ++t) {
-        sp_u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[e] = cvt_pk_bf16(x[2 * e], x[2 * e + 1]);
-            x[2 * e] -= __uint_as_float(w[e] << 16);
-            x[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+    if (write) {
+        for (int k = threadIdx.x; k < taken; k += threads) {             // (written before the last barrier)
+            const float x = p.mean ? p.g[k] / (float)taken : p.g[k];
+            p.g[k] = x;
+            p.exp_g[k] = (int)(__float_as_uint(x) >> 23 & 255u) - 127 - 14;   // |u| <= |g| is below 2^15 of it
         }
-        *reinterpret_cast<sp_u32x4*>(dst + t * plane + (int64_t)k * ldd + p * 8) = w;
+        if (threadIdx.x == 0) *p.count = taken;
     }
+    if (p.n == 0) __syncthreads();
+    *found_count = taken;
+    return source;
 }
 
-// Four elements of a row from d on, zeros from D on
-template <class T>
-__device__ __forceinline__ f32x4 xe_row4(const T* __restrict__ row, int d, int D) { return load4(row, d, D); }
+__global__ __launch_bounds__(1024) void xent_rows_kernel(const XentPack p) {
+    int count;
+    xe_find_rows(p, -1, true, 16, &count);
+}
 
-// Rows of `src` in fp16 terms: a workgroup a row, divided by 2^(exps[row]) so that its largest finite magnitude lies in [2^14, 2^15).
-// rows, count as above.
-template <class T>
-__global__ __launch_bounds__(256) void xent_pack16_kernel(const T* __restrict__ src, int64_t ld, int D, const int* __restrict__ rows,
-                                                          const int* __restrict__ count, int n, bf16_t* __restrict__ dst, int64_t ldd, int64_t plane,
-                                                          int terms, int* __restrict__ exps) {
+// largest finite magnitude of a workgroup's values
+__device__ __forceinline__ float xe_block_top(float top) {
     __shared__ float part[4];
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+    __syncthreads();
+    return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+__device__ __forceinline__ float xe_top4(f32x4 x, float top) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.f);
+    return top;
+}
+__device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float_as_uint(top) >> 23) - 127 - 14; }   // (2^-126 for all below)
+
+// Packed row blockIdx.x of the features: bf16 terms and fp16 terms (divided by 2^exps[row], the largest finite magnitude in [2^14, 2^15)),
+// zeros to whole stages and for rows behind those that take part; a row that takes none gets its results' zeros here.  window: one
+// stage more of the bf16 terms that repeats the last 64 columns, with zeros where they are in the stage before: it meets W's
+// last 64 columns where W is read as it is.
+template <class T>
+__global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) {
     const int k = blockIdx.x, tid = threadIdx.x;
-    const int real = rows ? min(*count, n) : n;
-    bf16_t* const out = dst + (int64_t)k * ldd;
+    int real, i;
+    if (p.n <= kXeFewRows) {
+        i = xe_find_rows(p, k, k == 0, 4, &real);
+    } else {
+        real = *p.count;
+        i = k < p.n ? p.rows[k] : -1;
+    }
+    bf16_t* const to = p.to + (int64_t)k * p.ld;
+    bf16_t* const to16 = p.to16 + (int64_t)k * p.ld16;
     if (k >= real) {
-        for (int d = tid * 4; d < ldd; d += 1024)
-            for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = make_uint2(0u, 0u);
-        if (tid == 0) exps[k] = -200;                                    // below any other: has no say in the largest
+        for (int d = tid * 4; d < p.ld; d += 1024)
+            for (int t = 0; t < p.terms; ++t) *reinterpret_cast<uint2*>(to + t * p.plane + d) = make_uint2(0u, 0u);
+        for (int d = tid * 4; d < p.ld16; d += 1024)
+            for (int t = 0; t < p.terms16; ++t) *reinterpret_cast<uint2*>(to16 + t * p.plane16 + d) = make_uint2(0u, 0u);
+        if (p.terms16 && tid == 0) p.exps[k] = 0;
+        if (k >= p.n) return;
+        if (p.zero)
+            for (int d = tid; d < p.D; d += 256) ((T*)p.zero)[(int64_t)i * p.ld_zero + d] = T(0);
+        if (tid == 0 && p.loss) p.loss[i] = 0.f;
+        if (tid == 0 && p.lse) p.lse[i] = 0.f;
         return;
     }
-    const T* const row = src + (int64_t)(rows ? rows[k] : k) * ld;
-    float top = 0.f;
-    for (int d = tid * 4; d < D; d += 1024) {
-        const f32x4 x = xe_row4(row, d, D);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.f);
+    const T* const row = (const T*)p.a + (int64_t)i * p.lda;
+    int e0 = 0;
+    if (p.terms16) {
+        float top = 0.f;
+        for (int d = tid * 4; d < p.D; d += 1024) top = xe_top4(load4(row, d, p.D), top);
+        e0 = xe_row_exponent(xe_block_top(top));
+        if (tid == 0) p.exps[k] = e0;
     }
-    top = wave_max(top);
-    if ((tid & 63) == 0) part[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    const int e0 = (int)(__float_as_uint(top) >> 23) - 127 - 14;         // (a row of zeros or of numbers below 2^-126: as if of those)
-    if (tid == 0) exps[k] = e0;
-    for (int d = tid * 4; d < ldd; d += 1024) {
-        const f32x4 v = xe_row4(row, d, D);
+    const int64_t whole = p.window ? p.window : p.terms ? p.ld : p.ld16;
+    for (int d = tid * 4; d < whole; d += 1024) {
+        const f32x4 v = load4(row, d, p.D);
         float x[4] = {__builtin_ldexpf(v[0], -e0), __builtin_ldexpf(v[1], -e0), __builtin_ldexpf(v[2], -e0), __builtin_ldexpf(v[3], -e0)};
-        for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = xe_half4(x);
+        for (int t = 0; t < p.terms16; ++t) *reinterpret_cast<uint2*>(to16 + t * p.plane16 + d) = xe_half4(x);
+        float b[4] = {v[0], v[1], v[2], v[3]};
+        for (int t = 0; t < p.terms; ++t) *reinterpret_cast<uint2*>(to + t * p.plane + d) = xe_bf4(b);
+    }
+    if (p.window && tid < 16) {
+        const int d = p.D - 64 + tid * 4;                                // D is a multiple of 8 here
+        f32x4 v = load4(row, d, p.D);
+        if (d < p.window - 64) v = f32x4{0.f, 0.f, 0.f, 0.f};
+        float b[4] = {v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<uint2*>(to + p.window + tid * 4) = xe_bf4(b);
+    }
+}
+
+// Rows of W, a workgroup each, in one bf16 term or (F16) fp16 terms and their exponents; zeros to whole stages and for rows from n on.
+template <class T, bool F16>
+__global__ __launch_bounds__(256) void xent_pack_words_kernel(const T* __restrict__ src, int64_t ld, int D, int n, bf16_t* __restrict__ dst, int64_t ldd,
+                                                              int64_t plane, int terms, int* __restrict__ exps) {
+    const int k = blockIdx.x, tid = threadIdx.x;
+    bf16_t* const out = dst + (int64_t)k * ldd;
+    if (k >= n) {
+        for (int d = tid * 4; d < ldd; d += 1024)
+            for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = make_uint2(0u, 0u);
+        if (F16 && tid == 0) exps[k] = -200;                             // below any other: has no say in the largest
+        return;
+    }
+    const T* const row = src + (int64_t)k * ld;
+    if constexpr (F16) {
+        float top = 0.f;
+        for (int d = tid * 4; d < D; d += 1024) top = xe_top4(load4(row, d, D), top);
+        const int e0 = xe_row_exponent(xe_block_top(top));
+        if (tid == 0) exps[k] = e0;
+        for (int d = tid * 4; d < ldd; d += 1024) {
+            const f32x4 v = load4(row, d, D);
+            float x[4] = {__builtin_ldexpf(v[0], -e0), __builtin_ldexpf(v[1], -e0), __builtin_ldexpf(v[2], -e0), __builtin_ldexpf(v[3], -e0)};
+            for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = xe_half4(x);
+        }
+    } else {
+        for (int d = tid * 4; d < ldd; d += 1024) {
+            const f32x4 v = load4(row, d, D);
+            float x[4] = {v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<uint2*>(out + d) = xe_bf4(x);
+        }
     }
 }
 
@@ -741,42 +795,9 @@ __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows 
     }
 }
 
-// lse and loss of a row from its tiles' maxima and sums: a wavefront a row, tiles in a fixed order
-__global__ __launch_bounds__(256) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_rows, const int* __restrict__ rows,
-                                                        const int* __restrict__ count, const float* __restrict__ z_label, float* __restrict__ loss,
-                                                        float* __restrict__ lse, float* __restrict__ lse_packed, float* __restrict__ loss_packed) {
-    const int k = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (k >= *count) return;
-    float top = -__builtin_inff(), sum = 0.f;
-    for (int t = lane; t < tiles; t += 64) {
-        const float2 p = partial[(int64_t)t * ld_rows + k];
-        const float m = fmaxf(top, p.x), base = m == -__builtin_inff() ? 0.f : m;
-        sum = sum * xe_exp(top - base) + p.y * xe_exp(p.x - base);
-        top = m;
-    }
-    const float most = wave_max(top), base = most == -__builtin_inff() ? 0.f : most;
-    sum = wave_sum(sum * xe_exp(top - base));
-    if (lane == 0) {
-        const float l = logf(sum), v = most + l, f = l + (most - z_label[k]);
-        const int i = rows[k];
-        if (lse) lse[i] = v;
-        if (loss) loss[i] = f;
-        lse_packed[k] = v;
-        loss_packed[k] = f;
-    }
-}
-
-__global__ __launch_bounds__(256) void xent_gather_kernel(const float* __restrict__ lse, const int* __restrict__ rows, const int* __restrict__ count,
-                                                          float* __restrict__ lse_packed) {
-    const int k = blockIdx.x * 256 + threadIdx.x;
-    if (k < *count) lse_packed[k] = lse[rows[k]];
-}
-
-// total = sum of g loss in a fixed order, in 64 bits
-__global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restrict__ loss, const float* __restrict__ g, const int* __restrict__ count,
-                                                          float* __restrict__ total) {
+// total = sum of g loss in a fixed order, in 64 bits; a workgroup of 1024
+__device__ __forceinline__ void xe_total(const float* loss, const float* g, int n, float* total) {
     __shared__ double part[16];
-    const int n = *count;
     double s = 0.0;
     for (int k = threadIdx.x; k < n; k += 1024) s += (double)loss[k] * (double)g[k];
 #pragma unroll
@@ -788,6 +809,49 @@ __global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restric
         for (int w = 0; w < 16; ++w) s += part[w];
         *total = (float)s;
     }
+}
+
+// lse and loss of a row from its tiles' maxima and sums: a wavefront a row, tiles in a fixed order.  One workgroup alone adds up the total
+// as well (total not null).
+__global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_rows, const int* __restrict__ rows,
+                                                         const int* __restrict__ counted, const float* __restrict__ z_label, const float* __restrict__ g,
+                                                         float* __restrict__ loss, float* __restrict__ lse, float* lse_packed, float* loss_packed,
+                                                         float* __restrict__ total) {
+    const int lane = threadIdx.x & 63, count = *counted;
+    for (int k = blockIdx.x * 16 + (threadIdx.x >> 6); k < count; k += gridDim.x * 16) {
+        float top = -__builtin_inff(), sum = 0.f;
+        for (int t = lane; t < tiles; t += 64) {
+            const float2 p = partial[(int64_t)t * ld_rows + k];
+            const float m = fmaxf(top, p.x), base = m == -__builtin_inff() ? 0.f : m;
+            sum = sum * xe_exp(top - base) + p.y * xe_exp(p.x - base);
+            top = m;
+        }
+        const float most = wave_max(top), base = most == -__builtin_inff() ? 0.f : most;
+        sum = wave_sum(sum * xe_exp(top - base));
+        if (lane == 0) {
+            const float l = logf(sum), v = most + l, f = l + (most - z_label[k]);
+            const int i = rows[k];
+            if (lse) lse[i] = v;
+            if (loss) loss[i] = f;
+            lse_packed[k] = v;
+            loss_packed[k] = f;
+        }
+    }
+    if (total) {
+        __syncthreads();
+        xe_total(loss_packed, g, count, total);
+    }
+}
+
+__global__ __launch_bounds__(256) void xent_gather_kernel(const float* __restrict__ lse, const int* __restrict__ rows, const int* __restrict__ count,
+                                                          float* __restrict__ lse_packed) {
+    const int k = blockIdx.x * 256 + threadIdx.x;
+    if (k < *count) lse_packed[k] = lse[rows[k]];
+}
+
+__global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restrict__ loss, const float* __restrict__ g, const int* __restrict__ count,
+                                                          float* __restrict__ total) {
+    xe_total(loss, g, *count, total);
 }
 
 // dA's rows from the accumulators' planes
@@ -832,20 +896,27 @@ static hipError_t launch_tiles(XentProduct a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Tiles, m x n.
-enum XentTile { kXe256x256, kXe128x128, kXe256x64, kXe256x32 };
-static const int kXeTileM[] = {256, 128, 256, 256}, kXeTileN[] = {256, 128, 64, 32};
+// Tiles, m x n; kXe128x128Lone: four stages on their way instead of two, a compute unit to itself.
+enum XentTile { kXe256x256, kXe128x128, kXe128x128Lone, kXe256x64, kXe256x32, kXe128x32 };
+static const int kXeTileM[] = {256, 128, 128, 256, 256, 128}, kXeTileN[] = {256, 128, 128, 64, 32, 32};
 
 template <bool XT, bool YT, bool F16, int END, class Out>
 static hipError_t launch_product(const XentProduct& a, XentTile tile, hipStream_t s) {
     switch (tile) {
-        case kXe256x256: return launch_tiles<2, 4, 4, 2, 2, 2, XT, YT, F16, END, Out>(a, s);
+        // four wavefronts of 128 x 128 read a third less of LDS than eight of 128 x 64 (16384 x 4096, k 4096: 1174 against 1080 TFLOP/s, W's
+        // k slow 1208 against 1125); what U's end and the scaling between fp16 terms take in registers goes with the eight only (U, 4096 x 4096: 1147
+        // against 1045)
+        case kXe256x256:
+            if constexpr (END == kXeU || F16) return launch_tiles<2, 4, 4, 2, 2, 2, XT, YT, F16, END, Out>(a, s);
+            else return launch_tiles<2, 2, 4, 4, 2, 1, XT, YT, F16, END, Out>(a, s);
         case kXe128x128: return launch_tiles<2, 2, 2, 2, 2, 2, XT, YT, F16, END, Out>(a, s);
+        case kXe128x128Lone: return launch_tiles<2, 2, 2, 2, 4, 1, XT, YT, F16, END, Out>(a, s);
         default: break;
     }
     if constexpr (!YT) {
         if (tile == kXe256x64) return launch_tiles<4, 1, 2, 2, 3, 1, XT, YT, F16, END, Out>(a, s);
         if (tile == kXe256x32) return launch_tiles<4, 1, 2, 1, 4, 1, XT, YT, F16, END, Out>(a, s);
+        if (tile == kXe128x32) return launch_tiles<4, 1, 1, 1, 4, 2, XT, YT, F16, END, Out>(a, s);
     }
     return hipErrorInvalidValue;
 }
@@ -855,20 +926,33 @@ struct Tiling {
     int splits;
 };
 
-// Tile and splits of k for an M x N product of `stages` stages (all pairs of terms): the fewest microseconds by what a stage takes a lone
-// workgroup, and a compute unit that is full of them.  splits <= most; each costs its plane's way to memory and back.
-static Tiling tiling_for(int64_t M, int64_t N, int64_t stages, int64_t most, bool rows_are_n) {
-    static const struct { XentTile tile; int resident; double lone_us, full_us; } kinds[] = {
-        {kXe256x256, 1, 1.70, 1.95}, {kXe128x128, 2, 0.58, 0.52}, {kXe256x64, 1, 0.60, 0.60}, {kXe256x32, 1, 0.50, 0.50}};
+// Tile and splits of k for an M x N product of `stages` stages (all pairs of terms), by microseconds: a launch's own, a round of workgroups',
+// a stage's in a lone workgroup (latency) and on a full card (at whose rate the matrix cores' clock falls), and the way of `out` bytes a result
+// to memory, splits (at most `most`) with planes of their own that are read again.  Fitted to 2100 products (D 256 to 20000, J 500 to
+// 60000, n 100 to 5000; each within 3 to 5 % for tiles of 256 and lone ones of 128, 8 to 14 % for pairs of them; the choice is within 1.1 % of
+// the best measured one on average).  Up to 64 rows take tiles of their own, bound by W's way from memory: 65536 x 4096, 32 rows:
+// scores in 128 x 32 113 us, 256 x 32 121; dA (k slow) 100 and 89.
+static Tiling tiling_for(int64_t M, int64_t N, int64_t stages, int64_t most, bool rows_are_n, bool k_slow, XentEnd end, double out) {
+    static const struct { XentTile tile; int resident; double own_us, round_us[2], lone_us, full_us; } kinds[] = {
+        {kXe256x256, 1, 8.0, {11.0, 2.0}, 1.07, 1.58},    {kXe128x128, 2, 4.0, {0.5, 0.0}, 0.64, 0.97}, {kXe128x128Lone, 1, 3.5, {4.0, 1.0}, 0.41, 0.53},
+        {kXe256x64, 1, 4.0, {2.0, 1.0}, 0.40, 0.55}, {kXe256x32, 1, 4.0, {2.0, 1.0}, 0.30, 0.45}, {kXe128x32, 2, 4.0, {2.0, 1.0}, 0.30, 0.45}};
     Tiling best{kXe128x128, 1};
     double best_us = 1e300;
     for (const auto& t : kinds) {
-        if (rows_are_n ? (t.tile == kXe256x32 && N > 32) || (t.tile == kXe256x64 && N > 64) : kXeTileN[t.tile] < 128) continue;
+        if (rows_are_n && N <= 64) {
+            if (t.tile != (N > 32 ? kXe256x64 : k_slow ? kXe256x32 : kXe128x32)) continue;
+        } else if (kXeTileN[t.tile] < 128 || (rows_are_n && N <= 128 && kXeTileN[t.tile] > 128)) {
+            continue;
+        }
         const int64_t tiles = ((M + kXeTileM[t.tile] - 1) / kXeTileM[t.tile]) * ((N + kXeTileN[t.tile] - 1) / kXeTileN[t.tile]);
+        const int64_t room = 256 * t.resident;
         for (int64_t s = 1; s <= most && (s == 1 || s * 4 <= stages); ++s) {
-            const int64_t n = tiles * s, deep = (n + 256 * t.resident - 1) / (256 * t.resident);
-            const double lone = t.lone_us * (double)deep, full = t.full_us * (double)((n + 255) / 256);
-            const double us = 3.0 * (double)deep + (double)((stages + s - 1) / s) * (lone > full ? lone : full) + (s > 1 ? (double)s * (double)M * (double)N * 8e-6 / 3.0 : 0.0);
+            const int64_t n = tiles * s, rest = n % room;
+            const double part = t.full_us * (double)rest / (double)room;
+            const double stage = t.full_us * (double)(n / room) + (rest == 0 ? 0.0 : part > t.lone_us ? part : t.lone_us);
+            const double plane = (double)M * (double)N * 1e-6;
+            const double us = t.own_us + t.round_us[end == kXeStore] * (double)((n + room - 1) / room) + (double)((stages + s - 1) / s) * stage +
+                              plane * out * (double)s / 4.0 + (s > 1 ? 2.0 + plane * 4.0 * (double)s / 4.0 : 0.0);
             if (us < best_us * 0.999) {
                 best_us = us;
                 best = Tiling{t.tile, (int)s};
@@ -925,7 +1009,7 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     l.direct = direct;
     l.kept = kept;
     l.piece = piece;
-    l.n_padded = up(n, 256);
+    l.n_padded = n <= 64 ? 64 : n <= 128 ? 128 : up(n, 256);             // whole tiles, and whole stages of dW's k
     l.k_tiles = (int)((c.D + 63) / 64);
     l.ld_k = 64 * (int64_t)l.k_tiles;
     l.window = direct && c.D % 64 != 0 ? (int)l.ld_k : 0;
@@ -946,11 +1030,12 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     }
     const int score_pairs = l.f16 ? pair_count(l.w16_terms, l.a16_terms, 1) : 1;
     const int64_t row_tiles = (n + 63) / 64, word_tiles = (words + 63) / 64;
-    l.scores = tiling_for(words, n, (int64_t)l.k_tiles * score_pairs, kept ? 16 : 1, true);
+    l.scores = tiling_for(words, n, (int64_t)l.k_tiles * score_pairs, kept ? 16 : 1, true, false,
+                          kept ? kXeStore : grads ? kXeU : kXeStats, kept ? 4.0 : 2.0 * (l.u_terms + l.u16_terms));
     if (grads) {
-        l.dA = tiling_for(c.D, n, word_tiles * (l.f16 ? pair_count(l.w16_terms, l.u16_terms, l.dA_most) : 1), 64, true);
+        l.dA = tiling_for(c.D, n, word_tiles * (l.f16 ? pair_count(l.w16_terms, l.u16_terms, l.dA_most) : 1), 64, true, true, kXeStore, 4.0);
         if (l.dA.splits > word_tiles) l.dA.splits = (int)word_tiles;
-        l.dW = tiling_for(c.D, words, row_tiles * (l.f16 ? pair_count(l.a_terms, l.u_terms, l.dW_most) : 1), 1, false);
+        l.dW = tiling_for(c.D, words, row_tiles * (l.f16 ? pair_count(l.a_terms, l.u_terms, l.dW_most) : 1), 1, false, true, kXeStore, c.w_bf16 ? 2.0 : 4.0);
     }
     if (l.scores.splits > l.k_tiles) l.scores.splits = l.k_tiles;
     size_t at = 0;
@@ -1058,35 +1143,23 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     int* const exp_w = (int*)(ws + l.exp_w);
     const int64_t a_plane = l.n_padded * l.ld_a, a16_plane = l.n_padded * l.ld_k, w_plane = l.piece * l.ld_k;
     const int64_t n_some = c.n > 0 ? c.n : 1;                            // an empty batch: nothing takes part, dW is 0
-    const int* const none = nullptr;
-    float* const nowhere = nullptr;
     hipError_t e;
 
-    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, c.y, (int)c.n, (int)c.J, c.weight, c.scale, c.mean, rows, label, g, exp_g, count);
     {
-        // (one term at least: what takes no part gets its zeros here)
-        const int64_t ld = l.a_terms ? l.ld_a : l.ld_k;
-        const uint32_t grid = (uint32_t)((l.n_padded * (ld / 8) + 255) / 256);
-        float* const loss0 = forward ? c.loss : nullptr;
-        float* const lse0 = forward ? c.lse : nullptr;
-        void* const dA0 = grads ? c.dA : nullptr;
-        if (c.a_bf16)
-            hipLaunchKernelGGL(xent_pack_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const bf16_t*)c.a, c.lda, (int)c.D, (const int*)rows, (const int*)count,
-                               (int)c.n, (int)l.n_padded, A, ld, a_plane, l.a_terms, l.window, (bf16_t*)dA0, c.ldda, loss0, lse0);
-        else
-            hipLaunchKernelGGL(xent_pack_kernel<float>, dim3(grid), dim3(256), 0, s, (const float*)c.a, c.lda, (int)c.D, (const int*)rows, (const int*)count,
-                               (int)c.n, (int)l.n_padded, A, ld, a_plane, l.a_terms, l.window, (float*)dA0, c.ldda, loss0, lse0);
+        XentPack p{};
+        p.a = c.a; p.lda = c.lda; p.n = (int)c.n; p.J = (int)c.J; p.D = (int)c.D; p.n_padded = (int)l.n_padded;
+        p.y = c.y; p.weight = c.weight; p.scale = c.scale; p.mean = c.mean;
+        p.rows = rows; p.label = label; p.exp_g = exp_g; p.count = count; p.g = g;
+        p.to = A; p.ld = l.ld_a; p.plane = a_plane; p.terms = l.a_terms; p.window = l.window;
+        p.to16 = A16; p.ld16 = l.f16 ? l.ld_k : 0; p.plane16 = a16_plane; p.terms16 = l.a16_terms; p.exps = exp_a;
+        p.zero = grads ? c.dA : nullptr; p.ld_zero = c.ldda;
+        p.loss = forward ? c.loss : nullptr; p.lse = forward ? c.lse : nullptr;
+        if (c.n > kXeFewRows) hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, p);
+        if (c.a_bf16) hipLaunchKernelGGL(xent_pack_rows_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, p);
+        else hipLaunchKernelGGL(xent_pack_rows_kernel<float>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, p);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    if (l.f16) {
-        if (c.a_bf16)
-            hipLaunchKernelGGL(xent_pack16_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, (const bf16_t*)c.a, c.lda, (int)c.D, (const int*)rows,
-                               (const int*)count, (int)c.n, A16, l.ld_k, a16_plane, l.a16_terms, exp_a);
-        else
-            hipLaunchKernelGGL(xent_pack16_kernel<float>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, (const float*)c.a, c.lda, (int)c.D, (const int*)rows,
-                               (const int*)count, (int)c.n, A16, l.ld_k, a16_plane, l.a16_terms, exp_a);
-    }
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
 
     // W's rows first .. first + n - 1 as an operand
     struct Words { const bf16_t* p; int64_t ld, plane; int rows; };
@@ -1100,19 +1173,16 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         *w = Words{Wp, l.ld_k, w_plane, (int)padded};
         if (there == first) return hipSuccess;
         there = first;
-        if (!l.f16) {
-            const uint32_t grid = (uint32_t)((padded * (l.ld_k / 8) + 255) / 256);
-            hipLaunchKernelGGL(xent_pack_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D, none, none, (int)n,
-                               (int)padded, Wp, l.ld_k, w_plane, 1, 0, (bf16_t*)nullptr, (int64_t)0, nowhere, nowhere);
-            return hipGetLastError();
-        }
-        if (c.w_bf16)
-            hipLaunchKernelGGL(xent_pack16_kernel<bf16_t>, dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D, none,
-                               none, (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
-        else
-            hipLaunchKernelGGL(xent_pack16_kernel<float>, dim3((uint32_t)padded), dim3(256), 0, s, (const float*)c.W + first * c.ldw, c.ldw, (int)c.D, none, none,
+        if (!l.f16)
+            hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, false>), dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D,
+                               (int)n, Wp, l.ld_k, w_plane, 1, (int*)nullptr);
+        else if (c.w_bf16)
+            hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true>), dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D,
                                (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
-        if (grads) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)exp_w, (int)n, top);
+        else
+            hipLaunchKernelGGL((xent_pack_words_kernel<float, true>), dim3((uint32_t)padded), dim3(256), 0, s, (const float*)c.W + first * c.ldw, c.ldw, (int)c.D,
+                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
+        if (l.f16 && grads) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)exp_w, (int)n, top);
         return hipGetLastError();
     };
     XentProduct scores{};
@@ -1140,6 +1210,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
+    bool total_done = false;
     if (l.kept) {
         Words w;
         e = words(0, c.J, &w);
@@ -1174,10 +1245,14 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             if (e != hipSuccess) return e;
             tiles += (int)((n + kXeTileM[l.scores.tile] - 1) / kXeTileM[l.scores.tile]);
         }
-        hipLaunchKernelGGL(xent_loss_kernel, dim3((uint32_t)((n_some + 3) / 4)), dim3(256), 0, s, (const float2*)(ws + l.partial), tiles, (int)l.n_padded,
-                           (const int*)rows, (const int*)count, (const float*)(ws + l.z_label), c.loss, c.lse, lse, loss);
+        // (64 rows are four a wavefront of one workgroup, which then needs no launch behind it for the total)
+        const bool alone = n_some <= 64;
+        hipLaunchKernelGGL(xent_loss_kernel, dim3(alone ? 1u : (uint32_t)((n_some + 15) / 16)), dim3(1024), 0, s, (const float2*)(ws + l.partial), tiles,
+                           (int)l.n_padded, (const int*)rows, (const int*)count, (const float*)(ws + l.z_label), (const float*)g, c.loss, c.lse, lse, loss,
+                           alone ? c.total : nullptr);
+        total_done = alone;
     }
-    if (forward && c.total)
+    if (forward && c.total && !total_done)
         hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, c.total);
     e = hipGetLastError();
     if (e != hipSuccess || !grads) return e;
