@@ -696,9 +696,10 @@ __global__ __launch_bounds__(1024) void xent_top_kernel(const int* __restrict__ 
 }
 
 struct XentRows {
-    const float* z;                          // [splits][..][ldz] scores of the one piece
+    const float* z;                          // [splits][..][ldz] scores of all words
     int64_t ldz, z_plane;
-    int splits, words, columns;              // columns: to the end of U's rows
+    int splits, words;
+    int first, columns;                      // U's words: from `first` on, `columns` of them with the padding of its rows (0: none)
     const int *rows, *label, *count;
     const float* g;
     float *loss, *lse;
@@ -707,14 +708,16 @@ struct XentRows {
     bf16_t *u, *u16;
     int64_t ldu, u_plane;
     int u_terms, u16_terms;
-    const int *exp_m, *exp_g, *exp_words;
+    const int *exp_m, *exp_g;                // of all words; of the rows
+    int* exp_words;                          // out: the largest of exp_m
     bool given;                              // lse_packed is there already
 };
 constexpr int kXeRowThreads = 512;
 
-// Kept scores: a workgroup a row, loss and U from one row of scores (read again for U: it is in the die's cache by then)
+// Kept scores: a workgroup a row, loss and a piece of U from one row of scores (read again for U: it is in the die's cache by then)
 __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows a) {
     __shared__ float red[2][kXeRowThreads / 64], z_label;
+    __shared__ int red_exp[kXeRowThreads / 64];
     const int k = blockIdx.x, tid = threadIdx.x, count = *a.count;
     bf16_t* const u = a.u + (int64_t)k * a.ldu;
     bf16_t* const u16 = a.u16 + (int64_t)k * a.ldu;
@@ -771,11 +774,26 @@ __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows 
             if (a.lse) a.lse[i] = lse;
             if (a.loss) a.loss[i] = f;
             a.loss_packed[k] = f;
+            a.lse_packed[k] = lse;                                       // (for the other pieces)
         }
     }
+    if (a.columns == 0) return;
     const float g = a.g[k];
-    const int en = a.u16_terms > 0 ? -a.exp_g[k] - *a.exp_words : 0;
-    for (int j = tid * 4; j < a.columns; j += kXeRowThreads * 4) {
+    int en = 0;
+    if (a.u16_terms > 0) {                                               // (every row finds it: a word's exponent is a third of its scores' bytes or less)
+        int m = -200;
+        for (int j = tid; j < a.words; j += kXeRowThreads) m = max(m, a.exp_m[j]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o, kWave));
+        if ((tid & 63) == 0) red_exp[tid >> 6] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kXeRowThreads / 64; ++w) m = max(m, red_exp[w]);
+        if (k == 0 && tid == 0) *a.exp_words = m;
+        en = -a.exp_g[k] - m;
+    }
+    for (int c = tid * 4; c < a.columns; c += kXeRowThreads * 4) {
+        const int j = a.first + c;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
         if (j < a.words) {
             const f32x4 s = scores(j);
@@ -787,11 +805,11 @@ __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows 
             }
         }
         if (a.u16_terms > 0) {
-            const int4 em = *reinterpret_cast<const int4*>(a.exp_m + j);
+            const int4 em = j < a.words ? *reinterpret_cast<const int4*>(a.exp_m + j) : make_int4(0, 0, 0, 0);
             float y[4] = {__builtin_ldexpf(x[0], en + em.x), __builtin_ldexpf(x[1], en + em.y), __builtin_ldexpf(x[2], en + em.z), __builtin_ldexpf(x[3], en + em.w)};
-            for (int t = 0; t < a.u16_terms; ++t) *reinterpret_cast<uint2*>(u16 + t * a.u_plane + j) = xe_half4(y);
+            for (int t = 0; t < a.u16_terms; ++t) *reinterpret_cast<uint2*>(u16 + t * a.u_plane + c) = xe_half4(y);
         }
-        for (int t = 0; t < a.u_terms; ++t) *reinterpret_cast<uint2*>(u + t * a.u_plane + j) = xe_bf4(x);
+        for (int t = 0; t < a.u_terms; ++t) *reinterpret_cast<uint2*>(u + t * a.u_plane + c) = xe_bf4(x);
     }
 }
 
@@ -820,10 +838,17 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restric
     const int lane = threadIdx.x & 63, count = *counted;
     for (int k = blockIdx.x * 16 + (threadIdx.x >> 6); k < count; k += gridDim.x * 16) {
         float top = -__builtin_inff(), sum = 0.f;
-        for (int t = lane; t < tiles; t += 64) {
-            const float2 p = partial[(int64_t)t * ld_rows + k];
-            const float m = fmaxf(top, p.x), base = m == -__builtin_inff() ? 0.f : m;
-            sum = sum * xe_exp(top - base) + p.y * xe_exp(p.x - base);
+        for (int t = lane; t < tiles; t += 512) {                        // eight on their way at a time
+            float2 p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = t + 64 * i < tiles ? partial[(int64_t)(t + 64 * i) * ld_rows + k] : make_float2(-__builtin_inff(), 0.f);
+            float m = top;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i].x);
+            const float base = m == -__builtin_inff() ? 0.f : m;
+            sum *= xe_exp(top - base);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += p[i].y * xe_exp(p[i].x - base);
             top = m;
         }
         const float most = wave_max(top), base = most == -__builtin_inff() ? 0.f : most;
@@ -983,12 +1008,12 @@ static int pair_count(int x_terms, int y_terms, int most) {
 
 namespace {
 constexpr int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-constexpr size_t kXePieceBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 30;   // of U and kept scores; of W's terms
+constexpr size_t kXePieceBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 30;   // of U, and of kept scores; of W's terms
 
 // What a call does and where it keeps it.
 struct Layout {
-    int64_t n_padded, piece, ld_k, ld_a, ld_acc;       // piece: words; ld_k: features to whole stages
-    bool f16, direct, kept;                            // fp16 terms (either operand fp32); W read as it is; scores of the one piece kept
+    int64_t n_padded, piece, ld_k, ld_a, ld_acc, ld_z; // piece: words; ld_k: features to whole stages
+    bool f16, direct, kept;                            // fp16 terms (either operand fp32); W read as it is; scores of all words kept
     int k_tiles, window;
     int a_terms, a16_terms, w16_terms, u_terms, u16_terms;
     int score_most, dA_most, dW_most;                  // pairs of terms
@@ -1055,11 +1080,12 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     l.top = take(4);
     if (l.f16) {
         l.exp_a = take((size_t)l.n_padded * 4);
-        l.exp_w = take((size_t)piece * 4);
+        l.exp_w = take((size_t)up(c.J, 256) * 4);
         l.a16 = take((size_t)l.a16_terms * l.n_padded * l.ld_k * 2);
     }
     if (l.a_terms) l.a = take((size_t)l.a_terms * l.n_padded * l.ld_a * 2);
-    if (kept) l.z = take((size_t)l.scores.splits * l.n_padded * piece * 4);
+    l.ld_z = up(c.J, 256);
+    if (kept) l.z = take((size_t)l.scores.splits * l.n_padded * l.ld_z * 4);
     else l.partial = take((size_t)(up(c.J, 256) / 128) * l.n_padded * 8);
     if (grads) {
         l.acc = take((size_t)l.dA.splits * n * l.ld_acc * 4);
@@ -1072,36 +1098,41 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
 }
 
 // Whether a call keeps its scores: they fit, and forming them again (or leaving most compute units idle) would take longer than their
-// way to memory and back.  A score costs 2 D flops a pair of terms again, at about 1 PFLOP/s, or some 12 bytes at 4 TB/s.
+// way to memory and back.  A score costs 2 D flops a pair of terms again, at about 1.1 PFLOP/s, or some 12 bytes at 4 TB/s.
 static bool keeps_scores(const XentCall& c, bool forward, bool grads) {
     const int64_t n = c.n > 0 ? c.n : 1, whole = up(c.J, 256);
-    if ((size_t)up(n, 256) * whole * 4 * 2 > kXePieceBytes) return false;
+    if ((size_t)up(n, 256) * whole * 4 > kXePieceBytes) return false;
     const int pairs = c.a_bf16 && c.w_bf16 ? 1 : c.a_bf16 || c.w_bf16 ? 2 : 3;
     const int64_t tiles = ((c.J + 127) / 128) * ((n + 127) / 128);
-    return n > 64 && ((forward && grads && c.D * pairs >= 1500) || (tiles < 200 && c.D * pairs >= 1500));
+    return n > 64 && c.D * pairs >= 1500 && ((forward && grads) || tiles < 200);
 }
 
 // The layout that a call on c's sizes takes within `bytes`; .bytes > bytes: there is none
 static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads, size_t bytes) {
     const int64_t whole = up(c.J, 256) / 256;
-    if (keeps_scores(c, forward, grads)) {
-        const Layout l = layout_of(c, direct, grads, true, whole * 256);
-        if (l.bytes <= bytes) return l;
+    for (int kept = keeps_scores(c, forward, grads); kept >= 0; --kept) {
+        if (!grads && direct) {
+            const Layout l = layout_of(c, true, false, kept != 0, whole * 256);
+            if (l.bytes <= bytes || !kept) return l;
+            continue;
+        }
+        // the most words whose U and whose W's terms stay within their bounds, and the whole within `bytes`
+        const Layout one = layout_of(c, direct, grads, kept != 0, 256);
+        const size_t u_bytes = (size_t)(one.u_terms + one.u16_terms) * one.n_padded * 512, w_bytes = direct ? 0 : (size_t)(one.f16 ? one.w16_terms : 1) * one.ld_k * 512;
+        int64_t lo = 1, hi = whole < (1 << 14) ? whole : (1 << 14);      // 32-bit offsets inside a tile: 2^22 words at most
+        if (u_bytes > 0 && hi > (int64_t)(kXePieceBytes / u_bytes)) hi = (int64_t)(kXePieceBytes / u_bytes);
+        if (w_bytes > 0 && hi > (int64_t)(kXeWordBytes / w_bytes)) hi = (int64_t)(kXeWordBytes / w_bytes);
+        if (layout_of(c, direct, grads, kept != 0, hi * 256).bytes <= bytes) lo = hi;    // (bytes may fall as pieces grow: fewer splits of dA)
+        while (lo < hi) {
+            const int64_t mid = (lo + hi + 1) / 2;
+            if (layout_of(c, direct, grads, kept != 0, mid * 256).bytes <= bytes) lo = mid; else hi = mid - 1;
+        }
+        const int64_t pieces = (whole + lo - 1) / lo;                    // evened out
+        Layout l = layout_of(c, direct, grads, kept != 0, (whole + pieces - 1) / pieces * 256);
+        if (l.bytes > bytes) l = layout_of(c, direct, grads, kept != 0, lo * 256);
+        if (l.bytes <= bytes || !kept) return l;
     }
-    if (!grads && direct) return layout_of(c, true, false, false, whole * 256);
-    // the most words whose U and whose W's terms stay within their bounds, and the whole within `bytes`
-    const Layout one = layout_of(c, direct, grads, false, 256);
-    const size_t u_bytes = (size_t)(one.u_terms + one.u16_terms) * one.n_padded * 512, w_bytes = direct ? 0 : (size_t)(one.f16 ? one.w16_terms : 1) * one.ld_k * 512;
-    int64_t lo = 1, hi = whole < (1 << 14) ? whole : (1 << 14);          // 32-bit offsets inside a tile: 2^22 words at most
-    if (u_bytes > 0 && hi > (int64_t)(kXePieceBytes / u_bytes)) hi = (int64_t)(kXePieceBytes / u_bytes);
-    if (w_bytes > 0 && hi > (int64_t)(kXeWordBytes / w_bytes)) hi = (int64_t)(kXeWordBytes / w_bytes);
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) / 2;
-        if (layout_of(c, direct, grads, false, mid * 256).bytes <= bytes) lo = mid; else hi = mid - 1;
-    }
-    const int64_t pieces = (whole + lo - 1) / lo;                        // evened out
-    const Layout l = layout_of(c, direct, grads, false, (whole + pieces - 1) / pieces * 256);
-    return l.bytes <= bytes ? l : layout_of(c, direct, grads, false, lo * 256);
+    return Layout{};                                                     // (not reached)
 }
 
 size_t xent_workspace(const XentCall& c, bool grads, bool least) {
@@ -1178,11 +1209,11 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
                                (int)n, Wp, l.ld_k, w_plane, 1, (int*)nullptr);
         else if (c.w_bf16)
             hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true>), dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D,
-                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
+                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w + first);
         else
             hipLaunchKernelGGL((xent_pack_words_kernel<float, true>), dim3((uint32_t)padded), dim3(256), 0, s, (const float*)c.W + first * c.ldw, c.ldw, (int)c.D,
-                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w);
-        if (l.f16 && grads) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)exp_w, (int)n, top);
+                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w + first);
+        if (l.f16 && grads && !l.kept) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)(exp_w + first), (int)n, top);
         return hipGetLastError();
     };
     XentProduct scores{};
@@ -1191,7 +1222,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     scores.last_x = l.window ? (int)c.D - 64 : 64 * (l.k_tiles - 1);
     scores.last_y = l.window ? l.window : 64 * (l.k_tiles - 1);
     scores.pairs = l.f16 ? pair_list(l.w16_terms, l.a16_terms, l.score_most, &scores.pair_x, &scores.pair_y) : 1;
-    scores.exp_m = exp_w; scores.exp_n = exp_a;
+    scores.exp_n = exp_a;
     scores.splits = 1;
     scores.count = count; scores.n_is_rows = true;
     scores.label = label; scores.ld_rows = (int)l.n_padded;
@@ -1200,6 +1231,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     auto scores_of = [&](int64_t first, int64_t n, const Words& w) {
         scores.x = w.p; scores.ldx = w.ld; scores.x_plane = w.plane; scores.x_rows = w.rows;
         scores.M = (int)n; scores.first_word = (int)first;
+        scores.exp_m = exp_w + first;
     };
     bf16_t* const U = (bf16_t*)(ws + l.u);
     bf16_t* const U16 = (bf16_t*)(ws + l.u16);
@@ -1211,26 +1243,35 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         if (e != hipSuccess) return e;
     }
     bool total_done = false;
-    if (l.kept) {
-        Words w;
-        e = words(0, c.J, &w);
-        if (e != hipSuccess) return e;
-        XentProduct p = scores;
-        p.x = w.p; p.ldx = w.ld; p.x_plane = w.plane; p.x_rows = w.rows;
-        p.M = (int)c.J;
-        p.splits = l.scores.splits;
-        p.out = ws + l.z; p.ldo = l.piece; p.out_plane = l.n_padded * l.piece; p.wide = true;
-        e = l.f16 ? launch_product<false, false, true, kXeStore, float>(p, l.scores.tile, s) : launch_product<false, false, false, kXeStore, float>(p, l.scores.tile, s);
-        if (e != hipSuccess) return e;
+    const int64_t pieces = (c.J + l.piece - 1) / l.piece;
+    // kept scores: the loss, and U's words from `first` on
+    auto rows_of = [&](int64_t first, bool given) {
         XentRows r{};
-        r.z = (const float*)(ws + l.z); r.ldz = l.piece; r.z_plane = p.out_plane; r.splits = l.scores.splits;
-        r.words = (int)c.J; r.columns = grads ? (int)l.piece : 0;
+        r.z = (const float*)(ws + l.z); r.ldz = l.ld_z; r.z_plane = l.n_padded * l.ld_z; r.splits = l.scores.splits;
+        r.words = (int)c.J; r.first = (int)first; r.columns = grads ? (int)l.piece : 0;
         r.rows = rows; r.label = label; r.count = count; r.g = g;
-        r.loss = forward ? c.loss : nullptr; r.lse = forward ? c.lse : nullptr; r.loss_packed = loss; r.lse_packed = lse;
+        r.loss = c.loss; r.lse = c.lse; r.loss_packed = loss; r.lse_packed = lse;
         r.u = U; r.u16 = U16; r.ldu = l.piece; r.u_plane = u_plane; r.u_terms = l.u_terms; r.u16_terms = l.u16_terms;
         r.exp_m = exp_w; r.exp_g = exp_g; r.exp_words = top;
-        r.given = !forward;
+        r.given = given;
         hipLaunchKernelGGL(xent_row_kernel, dim3((uint32_t)up(n_some, 64)), dim3(kXeRowThreads), 0, s, r);
+        return hipGetLastError();
+    };
+    if (l.kept) {
+        for (int64_t first = 0; first < c.J; first += l.piece) {
+            const int64_t n = c.J - first < l.piece ? c.J - first : l.piece;
+            Words w;
+            e = words(first, n, &w);
+            if (e != hipSuccess) return e;
+            scores_of(first, n, w);
+            XentProduct p = scores;
+            p.splits = l.scores.splits;
+            p.out = (float*)(ws + l.z) + first; p.ldo = l.ld_z; p.out_plane = l.n_padded * l.ld_z; p.wide = true;
+            e = l.f16 ? launch_product<false, false, true, kXeStore, float>(p, l.scores.tile, s) : launch_product<false, false, false, kXeStore, float>(p, l.scores.tile, s);
+            if (e != hipSuccess) return e;
+        }
+        e = rows_of((pieces - 1) * l.piece, !forward);
+        if (e != hipSuccess) return e;
     } else if (forward) {
         int tiles = 0;
         for (int64_t first = 0; first < c.J; first += l.piece) {
@@ -1258,13 +1299,15 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     if (e != hipSuccess || !grads) return e;
 
     // from the last piece back: its terms of W are still there
-    const int64_t pieces = (c.J + l.piece - 1) / l.piece;
     for (int64_t i = pieces - 1; i >= 0; --i) {
         const int64_t first = i * l.piece, n = c.J - first < l.piece ? c.J - first : l.piece;
         Words w;
         e = words(first, n, &w);
         if (e != hipSuccess) return e;
-        if (!l.kept) {
+        if (l.kept) {
+            if (i < pieces - 1) e = rows_of(first, true);
+            if (e != hipSuccess) return e;
+        } else {
             scores_of(first, n, w);
             scores.u = U; scores.u16 = U16; scores.ldu = l.piece; scores.u_plane = u_plane; scores.u_terms = l.u_terms; scores.u16_terms = l.u16_terms;
             scores.exp_g = exp_g; scores.exp_words = top;

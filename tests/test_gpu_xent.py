@@ -208,6 +208,14 @@ def test_pieces_of_the_vocabulary(dtype, w_dtype):
 
 
 @pytest.mark.parametrize("dtype,w_dtype", PAIRS)
+@pytest.mark.parametrize("two", [False, True])
+def test_pieces_of_long_features(two, dtype, w_dtype):
+    """The same where the scores are kept as long as the workspace holds them, in several pieces of U."""
+    for ws in (1e-9, 0.2, 0.35, 0.5, 0.7, 0.9, 1.0):
+        _run(150, 3000, 1600, dtype, w_dtype, 18, ws=ws, padded=0.1, two=two)
+
+
+@pytest.mark.parametrize("dtype,w_dtype", PAIRS)
 def test_two_calls_and_fewer_rows_than_the_head_takes(dtype, w_dtype):
     _run(77, 1500, 264, dtype, w_dtype, 11, rows=400, two=True, padded=0.2, weighted=True)
 
