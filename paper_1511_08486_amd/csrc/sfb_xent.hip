@@ -43,9 +43,9 @@ struct XentProduct {
     // kXeStats, kXeU
     const int* label;
     int first_word;                          // word of m = 0
-    float2* partial;                         // [m_tiles][ld_rows]
+    float2* partial;                         // [rows][ld_partial], from this product's first tile on
     float* z_label;
-    int ld_rows;
+    int ld_partial;
     const float *lse, *g;
     bf16_t *u, *u16;                         // [terms][..][ldu], in bf16 and fp16
     int64_t ldu, u_plane;
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
             const float base = top == -__builtin_inff() ? 0.f : top;
 #pragma unroll
             for (int w = 0; w < WGM; ++w) sum += red[w * BN + n].y * xe_exp(red[w * BN + n].x - base);
-            a.partial[(int64_t)(m0 / BM) * a.ld_rows + n0 + n] = make_float2(top, sum);
+            if (n0 + n < count) a.partial[(int64_t)(n0 + n) * a.ld_partial + m0 / BM] = make_float2(top, sum);
         }
     } else if constexpr (END == kXeU) {
         constexpr int PER = BM / 8;                                      // 16-byte pieces of an LDS row
@@ -513,7 +513,8 @@ struct XentPack {
     float scale;
     int mean;
     int *rows, *label, *exp_g, *count;       // what the later kernels read
-    float* g;
+    float *g, *lse_packed;
+    const float* lse_given;                  // or nullptr
     bf16_t *to, *to16;                       // bf16 and fp16 terms, [terms][n_padded][ld]
     int64_t ld, plane, ld16, plane16;
     int terms, terms16, window;
@@ -523,7 +524,7 @@ struct XentPack {
     float *loss, *lse;
 };
 
-// The rows that take part in front, in order, then the others; label, factor and its exponent of each of the former.  All threads of a
+// The rows that take part in front, in order, then the others; label, factor and its exponent, and a given lse, of each of the former.  All threads of a
 // workgroup of 64 `waves`; what is found of row `mine` of the packed order is returned (source row, or -1 behind n), and the count.
 __device__ __forceinline__ int xe_find_rows(const XentPack& p, int mine, bool write, int waves, int* found_count) {
     __shared__ int before[16], total, source;
@@ -555,6 +556,7 @@ __device__ __forceinline__ int xe_find_rows(const XentPack& p, int mine, bool wr
                 if (real) {
                     p.label[k] = lab;
                     p.g[k] = p.scale * (p.weight ? p.weight[i] : 1.f);
+                    if (p.lse_given) p.lse_packed[k] = p.lse_given[i];
                 }
             }
         }
@@ -579,7 +581,6 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(const XentPack p) {
     xe_find_rows(p, -1, true, 16, &count);
 }
 
-// largest finite magnitude of a workgroup's values
 __device__ __forceinline__ float xe_block_top(float top) {
     __shared__ float part[4];
     top = wave_max(top);
@@ -594,13 +595,57 @@ __device__ __forceinline__ float xe_top4(f32x4 x, float top) {
 }
 __device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float_as_uint(top) >> 23) - 127 - 14; }   // (2^-126 for all below)
 
-// Packed row blockIdx.x of the features: bf16 terms and fp16 terms (divided by 2^exps[row], the largest finite magnitude in [2^14, 2^15)),
-// zeros to whole stages and for rows behind those that take part; a row that takes none gets its results' zeros here.  window: one
-// stage more of the bf16 terms that repeats the last 64 columns, with zeros where they are in the stage before: it meets W's
-// last 64 columns where W is read as it is.
+// A row of D elements by a workgroup of 256: the first 4096 stay in registers between what looks them over and what takes them.
 template <class T>
-__global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) {
-    const int k = blockIdx.x, tid = threadIdx.x;
+struct XentRow {
+    f32x4 held[4];
+    const T* row;
+    int D;
+    __device__ __forceinline__ XentRow(const T* r, int d) : row(r), D(d) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) held[i] = load4(row, (int)threadIdx.x * 4 + 1024 * i, D);
+    }
+    // f(d, four elements from d on), d < whole; zeros from D on
+    template <class F>
+    __device__ __forceinline__ void each(int64_t whole, F f) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = (int)threadIdx.x * 4 + 1024 * i;
+            if (d < whole) f(d, held[i]);
+        }
+#pragma unroll 4
+        for (int d = (int)threadIdx.x * 4 + 4096; d < whole; d += 1024) f(d, load4(row, d, D));
+    }
+    // exponent that brings the largest finite magnitude into [2^14, 2^15) (2^-126 for all below)
+    __device__ __forceinline__ int exponent() const {
+        __shared__ float part[4];
+        float top = 0.f;
+        each(D, [&](int, f32x4 x) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.f);
+        });
+        top = wave_max(top);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        return (int)(__float_as_uint(top) >> 23) - 127 - 14;
+    }
+};
+__device__ __forceinline__ void xe_put16(bf16_t* to, int64_t plane, int terms, f32x4 v, int e0) {
+    float x[4] = {__builtin_ldexpf(v[0], -e0), __builtin_ldexpf(v[1], -e0), __builtin_ldexpf(v[2], -e0), __builtin_ldexpf(v[3], -e0)};
+    for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(to + t * plane) = xe_half4(x);
+}
+__device__ __forceinline__ void xe_put(bf16_t* to, int64_t plane, int terms, f32x4 v) {
+    float x[4] = {v[0], v[1], v[2], v[3]};
+    for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(to + t * plane) = xe_bf4(x);
+}
+
+// Packed row k of the features: bf16 terms and fp16 terms (divided by 2^exps[k]), zeros to whole stages and for rows behind those that take part; a
+// row that takes none gets its results' zeros here.  window: one stage more of the bf16 terms that repeats the last 64 columns, with zeros where
+// they are in the stage before: it meets W's last 64 columns where W is read as it is.
+template <class T>
+__device__ __forceinline__ void xe_pack_row(const XentPack& p, int k) {
+    const int tid = threadIdx.x;
     int real, i;
     if (p.n <= kXeFewRows) {
         i = xe_find_rows(p, k, k == 0, 4, &real);
@@ -611,10 +656,9 @@ __global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) {
     bf16_t* const to = p.to + (int64_t)k * p.ld;
     bf16_t* const to16 = p.to16 + (int64_t)k * p.ld16;
     if (k >= real) {
-        for (int d = tid * 4; d < p.ld; d += 1024)
-            for (int t = 0; t < p.terms; ++t) *reinterpret_cast<uint2*>(to + t * p.plane + d) = make_uint2(0u, 0u);
-        for (int d = tid * 4; d < p.ld16; d += 1024)
-            for (int t = 0; t < p.terms16; ++t) *reinterpret_cast<uint2*>(to16 + t * p.plane16 + d) = make_uint2(0u, 0u);
+        const f32x4 none{0.f, 0.f, 0.f, 0.f};
+        for (int d = tid * 4; d < p.ld; d += 1024) xe_put(to + d, p.plane, p.terms, none);
+        for (int d = tid * 4; d < p.ld16; d += 1024) xe_put(to16 + d, p.plane16, p.terms16, none);
         if (p.terms16 && tid == 0) p.exps[k] = 0;
         if (k >= p.n) return;
         if (p.zero)
@@ -623,61 +667,62 @@ __global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) {
         if (tid == 0 && p.lse) p.lse[i] = 0.f;
         return;
     }
-    const T* const row = (const T*)p.a + (int64_t)i * p.lda;
+    const T* const src = (const T*)p.a + (int64_t)i * p.lda;
+    const XentRow<T> row(src, p.D);
     int e0 = 0;
     if (p.terms16) {
-        float top = 0.f;
-        for (int d = tid * 4; d < p.D; d += 1024) top = xe_top4(load4(row, d, p.D), top);
-        e0 = xe_row_exponent(xe_block_top(top));
+        e0 = row.exponent();
         if (tid == 0) p.exps[k] = e0;
     }
-    const int64_t whole = p.window ? p.window : p.terms ? p.ld : p.ld16;
-    for (int d = tid * 4; d < whole; d += 1024) {
-        const f32x4 v = load4(row, d, p.D);
-        float x[4] = {__builtin_ldexpf(v[0], -e0), __builtin_ldexpf(v[1], -e0), __builtin_ldexpf(v[2], -e0), __builtin_ldexpf(v[3], -e0)};
-        for (int t = 0; t < p.terms16; ++t) *reinterpret_cast<uint2*>(to16 + t * p.plane16 + d) = xe_half4(x);
-        float b[4] = {v[0], v[1], v[2], v[3]};
-        for (int t = 0; t < p.terms; ++t) *reinterpret_cast<uint2*>(to + t * p.plane + d) = xe_bf4(b);
-    }
+    row.each(p.window ? p.window : p.terms ? p.ld : p.ld16, [&](int d, f32x4 v) {
+        xe_put16(to16 + d, p.plane16, p.terms16, v, e0);
+        xe_put(to + d, p.plane, p.terms, v);
+    });
     if (p.window && tid < 16) {
         const int d = p.D - 64 + tid * 4;                                // D is a multiple of 8 here
-        f32x4 v = load4(row, d, p.D);
+        f32x4 v = load4(src, d, p.D);
         if (d < p.window - 64) v = f32x4{0.f, 0.f, 0.f, 0.f};
-        float b[4] = {v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<uint2*>(to + p.window + tid * 4) = xe_bf4(b);
+        xe_put(to + p.window + tid * 4, 0, 1, v);
     }
 }
 
-// Rows of W, a workgroup each, in one bf16 term or (F16) fp16 terms and their exponents; zeros to whole stages and for rows from n on.
+struct XentWords {
+    const void* w;
+    int64_t ld;
+    int D, n;
+    bf16_t* to;
+    int64_t ldd, plane;
+    int terms;
+    int* exps;
+};
+// Row k of W's piece in one bf16 term or (F16) fp16 terms and its exponent; zeros to whole stages and for rows from n on.
 template <class T, bool F16>
-__global__ __launch_bounds__(256) void xent_pack_words_kernel(const T* __restrict__ src, int64_t ld, int D, int n, bf16_t* __restrict__ dst, int64_t ldd,
-                                                              int64_t plane, int terms, int* __restrict__ exps) {
-    const int k = blockIdx.x, tid = threadIdx.x;
-    bf16_t* const out = dst + (int64_t)k * ldd;
-    if (k >= n) {
-        for (int d = tid * 4; d < ldd; d += 1024)
-            for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = make_uint2(0u, 0u);
-        if (F16 && tid == 0) exps[k] = -200;                             // below any other: has no say in the largest
+__device__ __forceinline__ void xe_pack_word(const XentWords& p, int k) {
+    bf16_t* const out = p.to + (int64_t)k * p.ldd;
+    if (k >= p.n) {
+        for (int d = threadIdx.x * 4; d < p.ldd; d += 1024) xe_put(out + d, p.plane, p.terms, f32x4{0.f, 0.f, 0.f, 0.f});
+        if (F16 && threadIdx.x == 0) p.exps[k] = -200;                   // below any other: has no say in the largest
         return;
     }
-    const T* const row = src + (int64_t)k * ld;
+    const XentRow<T> row((const T*)p.w + (int64_t)k * p.ld, p.D);
     if constexpr (F16) {
-        float top = 0.f;
-        for (int d = tid * 4; d < D; d += 1024) top = xe_top4(load4(row, d, D), top);
-        const int e0 = xe_row_exponent(xe_block_top(top));
-        if (tid == 0) exps[k] = e0;
-        for (int d = tid * 4; d < ldd; d += 1024) {
-            const f32x4 v = load4(row, d, D);
-            float x[4] = {__builtin_ldexpf(v[0], -e0), __builtin_ldexpf(v[1], -e0), __builtin_ldexpf(v[2], -e0), __builtin_ldexpf(v[3], -e0)};
-            for (int t = 0; t < terms; ++t) *reinterpret_cast<uint2*>(out + t * plane + d) = xe_half4(x);
-        }
+        const int e0 = row.exponent();
+        if (threadIdx.x == 0) p.exps[k] = e0;
+        row.each(p.ldd, [&](int d, f32x4 v) { xe_put16(out + d, p.plane, p.terms, v, e0); });
     } else {
-        for (int d = tid * 4; d < ldd; d += 1024) {
-            const f32x4 v = load4(row, d, D);
-            float x[4] = {v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<uint2*>(out + d) = xe_bf4(x);
-        }
+        row.each(p.ldd, [&](int d, f32x4 v) { xe_put(out + d, p.plane, 1, v); });
     }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) { xe_pack_row<T>(p, blockIdx.x); }
+template <class T, bool F16>
+__global__ __launch_bounds__(256) void xent_pack_words_kernel(const XentWords w) { xe_pack_word<T, F16>(w, blockIdx.x); }
+// The rows and the first piece's words in one launch
+template <class TA, class TW, bool F16>
+__global__ __launch_bounds__(256) void xent_pack_both_kernel(const XentPack p, const XentWords w) {
+    if ((int)blockIdx.x < p.n_padded) xe_pack_row<TA>(p, blockIdx.x);
+    else xe_pack_word<TW, F16>(w, (int)blockIdx.x - p.n_padded);
 }
 
 // The largest of a piece's exponents
@@ -831,7 +876,7 @@ __device__ __forceinline__ void xe_total(const float* loss, const float* g, int 
 
 // lse and loss of a row from its tiles' maxima and sums: a wavefront a row, tiles in a fixed order.  One workgroup alone adds up the total
 // as well (total not null).
-__global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_rows, const int* __restrict__ rows,
+__global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_partial, const int* __restrict__ rows,
                                                          const int* __restrict__ counted, const float* __restrict__ z_label, const float* __restrict__ g,
                                                          float* __restrict__ loss, float* __restrict__ lse, float* lse_packed, float* loss_packed,
                                                          float* __restrict__ total) {
@@ -841,7 +886,7 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restric
         for (int t = lane; t < tiles; t += 512) {                        // eight on their way at a time
             float2 p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = t + 64 * i < tiles ? partial[(int64_t)(t + 64 * i) * ld_rows + k] : make_float2(-__builtin_inff(), 0.f);
+            for (int i = 0; i < 8; ++i) p[i] = t + 64 * i < tiles ? partial[(int64_t)k * ld_partial + t + 64 * i] : make_float2(-__builtin_inff(), 0.f);
             float m = top;
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i].x);
@@ -866,12 +911,6 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restric
         __syncthreads();
         xe_total(loss_packed, g, count, total);
     }
-}
-
-__global__ __launch_bounds__(256) void xent_gather_kernel(const float* __restrict__ lse, const int* __restrict__ rows, const int* __restrict__ count,
-                                                          float* __restrict__ lse_packed) {
-    const int k = blockIdx.x * 256 + threadIdx.x;
-    if (k < *count) lse_packed[k] = lse[rows[k]];
 }
 
 __global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restrict__ loss, const float* __restrict__ g, const int* __restrict__ count,
@@ -1012,7 +1051,7 @@ constexpr size_t kXePieceBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 
 
 // What a call does and where it keeps it.
 struct Layout {
-    int64_t n_padded, piece, ld_k, ld_a, ld_acc, ld_z; // piece: words; ld_k: features to whole stages
+    int64_t n_padded, piece, ld_k, ld_a, ld_acc, ld_z, ld_partial; // piece: words; ld_k: features to whole stages
     bool f16, direct, kept;                            // fp16 terms (either operand fp32); W read as it is; scores of all words kept
     int k_tiles, window;
     int a_terms, a16_terms, w16_terms, u_terms, u16_terms;
@@ -1086,7 +1125,8 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     if (l.a_terms) l.a = take((size_t)l.a_terms * l.n_padded * l.ld_a * 2);
     l.ld_z = up(c.J, 256);
     if (kept) l.z = take((size_t)l.scores.splits * l.n_padded * l.ld_z * 4);
-    else l.partial = take((size_t)(up(c.J, 256) / 128) * l.n_padded * 8);
+    l.ld_partial = up(c.J, 256) / 128;
+    if (!kept) l.partial = take((size_t)l.ld_partial * n * 8);
     if (grads) {
         l.acc = take((size_t)l.dA.splits * n * l.ld_acc * 4);
         l.u = take((size_t)l.u_terms * l.n_padded * piece * 2);
@@ -1176,43 +1216,50 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     const int64_t n_some = c.n > 0 ? c.n : 1;                            // an empty batch: nothing takes part, dW is 0
     hipError_t e;
 
+    XentPack pack;
     {
         XentPack p{};
         p.a = c.a; p.lda = c.lda; p.n = (int)c.n; p.J = (int)c.J; p.D = (int)c.D; p.n_padded = (int)l.n_padded;
         p.y = c.y; p.weight = c.weight; p.scale = c.scale; p.mean = c.mean;
         p.rows = rows; p.label = label; p.exp_g = exp_g; p.count = count; p.g = g;
+        p.lse_packed = lse; p.lse_given = forward ? nullptr : c.lse;
         p.to = A; p.ld = l.ld_a; p.plane = a_plane; p.terms = l.a_terms; p.window = l.window;
         p.to16 = A16; p.ld16 = l.f16 ? l.ld_k : 0; p.plane16 = a16_plane; p.terms16 = l.a16_terms; p.exps = exp_a;
         p.zero = grads ? c.dA : nullptr; p.ld_zero = c.ldda;
         p.loss = forward ? c.loss : nullptr; p.lse = forward ? c.lse : nullptr;
-        if (c.n > kXeFewRows) hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, p);
-        if (c.a_bf16) hipLaunchKernelGGL(xent_pack_rows_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, p);
-        else hipLaunchKernelGGL(xent_pack_rows_kernel<float>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, p);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        pack = p;
     }
+    if (c.n > kXeFewRows) hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, pack);
 
-    // W's rows first .. first + n - 1 as an operand
+    // W's rows first .. first + n - 1 as an operand; the first call packs the features as well
     struct Words { const bf16_t* p; int64_t ld, plane; int rows; };
     int64_t there = -1;                                                  // the piece whose terms are in the workspace
     auto words = [&](int64_t first, int64_t n, Words* w) -> hipError_t {
+        const bool rows_too = there < 0;
         if (direct) {
             *w = Words{(const bf16_t*)c.W + first * c.ldw, c.ldw, 0, (int)n};
-            return hipSuccess;
+            if (rows_too) hipLaunchKernelGGL(xent_pack_rows_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, pack);
+            there = 0;
+            return rows_too ? hipGetLastError() : hipSuccess;
         }
         const int64_t padded = up(n, 64);
         *w = Words{Wp, l.ld_k, w_plane, (int)padded};
         if (there == first) return hipSuccess;
         there = first;
-        if (!l.f16)
-            hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, false>), dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D,
-                               (int)n, Wp, l.ld_k, w_plane, 1, (int*)nullptr);
-        else if (c.w_bf16)
-            hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true>), dim3((uint32_t)padded), dim3(256), 0, s, (const bf16_t*)c.W + first * c.ldw, c.ldw, (int)c.D,
-                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w + first);
-        else
-            hipLaunchKernelGGL((xent_pack_words_kernel<float, true>), dim3((uint32_t)padded), dim3(256), 0, s, (const float*)c.W + first * c.ldw, c.ldw, (int)c.D,
-                               (int)n, Wp, l.ld_k, w_plane, l.w16_terms, exp_w + first);
+        const XentWords x{(const char*)c.W + (size_t)first * c.ldw * (c.w_bf16 ? 2 : 4), c.ldw, (int)c.D, (int)n, Wp, l.ld_k, w_plane, l.f16 ? l.w16_terms : 1,
+                          l.f16 ? exp_w + first : nullptr};
+        if (rows_too) {
+            const dim3 grid((uint32_t)(l.n_padded + padded)), block(256);
+            if (!l.f16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, bf16_t, false>), grid, block, 0, s, pack, x);
+            else if (c.w_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<float, bf16_t, true>), grid, block, 0, s, pack, x);
+            else if (c.a_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, float, true>), grid, block, 0, s, pack, x);
+            else hipLaunchKernelGGL((xent_pack_both_kernel<float, float, true>), grid, block, 0, s, pack, x);
+        } else {
+            const dim3 grid((uint32_t)padded), block(256);
+            if (!l.f16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, false>), grid, block, 0, s, x);
+            else if (c.w_bf16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true>), grid, block, 0, s, x);
+            else hipLaunchKernelGGL((xent_pack_words_kernel<float, true>), grid, block, 0, s, x);
+        }
         if (l.f16 && grads && !l.kept) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)(exp_w + first), (int)n, top);
         return hipGetLastError();
     };
@@ -1225,7 +1272,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     scores.exp_n = exp_a;
     scores.splits = 1;
     scores.count = count; scores.n_is_rows = true;
-    scores.label = label; scores.ld_rows = (int)l.n_padded;
+    scores.label = label; scores.ld_partial = (int)l.ld_partial;
     scores.z_label = (float*)(ws + l.z_label);
     scores.lse = lse; scores.g = g;
     auto scores_of = [&](int64_t first, int64_t n, const Words& w) {
@@ -1237,11 +1284,6 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     bf16_t* const U16 = (bf16_t*)(ws + l.u16);
     const int64_t u_plane = l.n_padded * l.piece, acc_plane = n_some * l.ld_acc;
 
-    if (!forward) {
-        hipLaunchKernelGGL(xent_gather_kernel, dim3((uint32_t)((n_some + 255) / 256)), dim3(256), 0, s, (const float*)c.lse, (const int*)rows, (const int*)count, lse);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
     bool total_done = false;
     const int64_t pieces = (c.J + l.piece - 1) / l.piece;
     // kept scores: the loss, and U's words from `first` on
@@ -1280,7 +1322,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             e = words(first, n, &w);
             if (e != hipSuccess) return e;
             scores_of(first, n, w);
-            scores.partial = (float2*)(ws + l.partial) + (int64_t)tiles * l.n_padded;
+            scores.partial = (float2*)(ws + l.partial) + tiles;
             e = l.f16 ? launch_product<false, false, true, kXeStats, float>(scores, l.scores.tile, s)
                       : launch_product<false, false, false, kXeStats, float>(scores, l.scores.tile, s);
             if (e != hipSuccess) return e;
@@ -1289,7 +1331,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         // (64 rows are four a wavefront of one workgroup, which then needs no launch behind it for the total)
         const bool alone = n_some <= 64;
         hipLaunchKernelGGL(xent_loss_kernel, dim3(alone ? 1u : (uint32_t)((n_some + 15) / 16)), dim3(1024), 0, s, (const float2*)(ws + l.partial), tiles,
-                           (int)l.n_padded, (const int*)rows, (const int*)count, (const float*)(ws + l.z_label), (const float*)g, c.loss, c.lse, lse, loss,
+                           (int)l.ld_partial, (const int*)rows, (const int*)count, (const float*)(ws + l.z_label), (const float*)g, c.loss, c.lse, lse, loss,
                            alone ? c.total : nullptr);
         total_done = alone;
     }
