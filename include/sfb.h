@@ -304,14 +304,15 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
  * with w_i = weight[i] or 1, and f = scale, or scale divided by the number of rows that take part (mean != 0).  A row whose label lies outside
  * [0, J) takes no part: its loss, lse and row of dA are 0, and its features are not looked at (they may be anything).  Rows n and
  * beyond of no output are touched; n = 0 is an empty batch (total = 0, dW = 0).
- *   W, a        each in its own dtype: bf16 products are taken as they are, fp32 operands as three bf16 terms (exact below 3.38e38; what is
- *               beyond, or below 2^-109 in part, is rounded to bf16's range), sums in fp32
- *   dA, dW      in the types of a and W, or NULL: not wanted.  With both in bf16 U is rounded to bf16 on the way (as large an error again as the
- *               results' own rounding); otherwise it is kept in three terms
+ *   W, a        each in its own dtype: bf16 products are taken as they are, fp32 operands as two fp16 terms of every row divided by its own
+ *               power of two (22 bits of a value above 2^-29 of its row's largest), for dW as three bf16 terms (exact); sums in fp32
+ *   dA, dW      in the types of a and W, or NULL: not wanted.  With both in bf16 U is rounded to bf16 on the way, before f is applied (with
+ *               the results' own rounding 1.2 times the error of that alone, 1.5 with weights of any size); otherwise it is kept in
+ *               more terms
  *   loss, lse, total, weight   DEVICE fp32, NULL: not wanted (lse is needed by sfb_xent_gradients, which reads what sfb_xent_loss left)
  *   ws          DEVICE, 256-byte aligned; it belongs to the call until that has run: calls that may overlap in time, replays of captured
  *               ones included, need one each.  sfb_xent_workspace_bytes: the least a call on up to P*B rows can take, and as much as
- *               speeds it up (pieces of some 256 MB).  grads != 0: of the calls that form gradients.
+ *               speeds it up (pieces of some 512 MB).  grads != 0: of the calls that form gradients.
  * sfb_xent_gradients and sfb_xent_loss_and_gradients give the same gradients, to rounding.  Results do not depend on the order in which
  * anything runs.  No two of the arrays may overlap.
  * SFB_EINVAL: a null pointer that is needed, a scale that is not finite, ws not aligned; SFB_ESHAPE: a leading dimension shorter than a row, n outside

@@ -1,7 +1,7 @@
 // Softmax cross entropy of a linear head, z_i = W a_i, without the N x J scores in memory, and its gradients.
 //
 //   lse_i = log sum_j exp(z_ij)       loss_i = lse_i - z_i,y(i)
-//   u_ij  = g_i (exp(z_ij - lse_i) - [j = y(i)])         dA = U W         dW = U^T A
+//   u_ij  = w_i (exp(z_ij - lse_i) - [j = y(i)])         dA = f U W       dW = f U^T A      (w: the rows' weights, f: the scale)
 // Rows whose label is outside [0, J) take no part: the others are packed to the front (by their labels, on the device), so a padded batch
 // costs what its real rows cost, and what stands in the padding is never multiplied.
 //
@@ -15,7 +15,7 @@
 // fp32 operands go in terms of 16 bits, a longer k to the kernel, the small products first:
 //   scores and dA  two fp16 terms of every row divided by its own power of two, x = 2^e (h + l / 2048): 22 bits of every value above 2^-29 of its
 //                  row's largest, and three products (two with one bf16 operand, which is one fp16 term).  Of dA's contraction W's exponents
-//                  are in U, and U's rows are divided by what their factor g_i bounds them by.  A bf16 dA takes one term of each (2^-12).
+//                  are in U, and U's rows are divided by what their weight bounds them by.  A bf16 dA takes one term of each (2^-12).
 //   dW             three bf16 terms (exact) and six products (three with bf16 features): along its contraction, the rows, the factors of a
 //                  rare word may all be below 2^-40 of a label's, and must not be rounded by that.
 // Small problems, whose scores and U fit the workspace beside each other, keep the scores of the one piece instead of forming them twice.
@@ -54,6 +54,7 @@ struct XentProduct {
     // kXeStore
     void* out;
     int64_t ldo, out_plane;                  // out_plane: between splits
+    const float* factor;                     // of the results
     const float* add;                        // fp32, or nullptr
     int64_t ld_add;
     const int* row_map;                      // row of out for n, or nullptr
@@ -446,6 +447,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
         constexpr int PER = BM / 4;
         const int n_most = a.n_is_rows ? min(a.N, count) : a.N;
         Out* const out = reinterpret_cast<Out*>(a.out) + split * a.out_plane;
+        const float factor = a.factor ? *a.factor : 1.f;
         const float* const add = a.add ? a.add + split * a.out_plane : nullptr;
 #pragma unroll
         for (int j0 = 0; j0 < NT; j0 += JR) {
@@ -472,6 +474,8 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
                 if (n >= n_most || m >= a.M) continue;
                 f32x4 lo = *reinterpret_cast<const f32x4*>(xe_lds + row * (BM * 4) + (((2 * p8) ^ (row & 15)) << 4));
                 f32x4 hi = *reinterpret_cast<const f32x4*>(xe_lds + row * (BM * 4) + (((2 * p8 + 1) ^ (row & 15)) << 4));
+                lo *= factor;
+                hi *= factor;
                 if (add) {
                     const float* p = add + (int64_t)n * a.ld_add + m;    // (rows of the accumulators are whole multiples of 8)
                     lo += *reinterpret_cast<const f32x4*>(p);
@@ -513,7 +517,7 @@ struct XentPack {
     float scale;
     int mean;
     int *rows, *label, *exp_g, *count;       // what the later kernels read
-    float *g, *lse_packed;
+    float *g, *lse_packed, *factor;          // g: the rows' weights; factor: scale, or scale / count
     const float* lse_given;                  // or nullptr
     bf16_t *to, *to16;                       // bf16 and fp16 terms, [terms][n_padded][ld]
     int64_t ld, plane, ld16, plane16;
@@ -524,7 +528,7 @@ struct XentPack {
     float *loss, *lse;
 };
 
-// The rows that take part in front, in order, then the others; label, factor and its exponent, and a given lse, of each of the former.  All threads of a
+// The rows that take part in front, in order, then the others; label, weight and its exponent, and a given lse, of each of the former.  All threads of a
 // workgroup of 64 `waves`; what is found of row `mine` of the packed order is returned (source row, or -1 behind n), and the count.
 __device__ __forceinline__ int xe_find_rows(const XentPack& p, int mine, bool write, int waves, int* found_count) {
     __shared__ int before[16], total, source;
@@ -555,7 +559,7 @@ __device__ __forceinline__ int xe_find_rows(const XentPack& p, int mine, bool wr
                 p.rows[at] = i;
                 if (real) {
                     p.label[k] = lab;
-                    p.g[k] = p.scale * (p.weight ? p.weight[i] : 1.f);
+                    p.g[k] = p.weight ? p.weight[i] : 1.f;
                     if (p.lse_given) p.lse_packed[k] = p.lse_given[i];
                 }
             }
@@ -565,11 +569,12 @@ __device__ __forceinline__ int xe_find_rows(const XentPack& p, int mine, bool wr
     }
     if (write) {
         for (int k = threadIdx.x; k < taken; k += threads) {             // (written before the last barrier)
-            const float x = p.mean ? p.g[k] / (float)taken : p.g[k];
-            p.g[k] = x;
-            p.exp_g[k] = (int)(__float_as_uint(x) >> 23 & 255u) - 127 - 14;   // |u| <= |g| is below 2^15 of it
+            p.exp_g[k] = (int)(__float_as_uint(p.g[k]) >> 23 & 255u) - 127 - 14;   // |u| <= |g| is below 2^15 of it
         }
-        if (threadIdx.x == 0) *p.count = taken;
+        if (threadIdx.x == 0) {
+            *p.count = taken;
+            *p.factor = p.mean && taken > 0 ? p.scale / (float)taken : p.scale;
+        }
     }
     if (p.n == 0) __syncthreads();
     *found_count = taken;
@@ -858,8 +863,8 @@ __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows 
     }
 }
 
-// total = sum of g loss in a fixed order, in 64 bits; a workgroup of 1024
-__device__ __forceinline__ void xe_total(const float* loss, const float* g, int n, float* total) {
+// total = f sum of g loss in a fixed order, in 64 bits; a workgroup of 1024
+__device__ __forceinline__ void xe_total(const float* loss, const float* g, int n, const float* factor, float* total) {
     __shared__ double part[16];
     double s = 0.0;
     for (int k = threadIdx.x; k < n; k += 1024) s += (double)loss[k] * (double)g[k];
@@ -870,7 +875,7 @@ __device__ __forceinline__ void xe_total(const float* loss, const float* g, int 
     if (threadIdx.x == 0) {
         s = 0.0;
         for (int w = 0; w < 16; ++w) s += part[w];
-        *total = (float)s;
+        *total = (float)(s * (double)*factor);
     }
 }
 
@@ -879,7 +884,7 @@ __device__ __forceinline__ void xe_total(const float* loss, const float* g, int 
 __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_partial, const int* __restrict__ rows,
                                                          const int* __restrict__ counted, const float* __restrict__ z_label, const float* __restrict__ g,
                                                          float* __restrict__ loss, float* __restrict__ lse, float* lse_packed, float* loss_packed,
-                                                         float* __restrict__ total) {
+                                                         const float* __restrict__ factor, float* __restrict__ total) {
     const int lane = threadIdx.x & 63, count = *counted;
     for (int k = blockIdx.x * 16 + (threadIdx.x >> 6); k < count; k += gridDim.x * 16) {
         float top = -__builtin_inff(), sum = 0.f;
@@ -909,13 +914,13 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restric
     }
     if (total) {
         __syncthreads();
-        xe_total(loss_packed, g, count, total);
+        xe_total(loss_packed, g, count, factor, total);
     }
 }
 
 __global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restrict__ loss, const float* __restrict__ g, const int* __restrict__ count,
-                                                          float* __restrict__ total) {
-    xe_total(loss, g, *count, total);
+                                                          const float* __restrict__ factor, float* __restrict__ total) {
+    xe_total(loss, g, *count, factor, total);
 }
 
 // dA's rows from the accumulators' planes
@@ -1047,7 +1052,7 @@ static int pair_count(int x_terms, int y_terms, int most) {
 
 namespace {
 constexpr int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-constexpr size_t kXePieceBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 30;   // of U, and of kept scores; of W's terms
+constexpr size_t kXePieceBytes = (size_t)512 << 20, kXeScoreBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 30;   // of U, kept scores and W's terms
 
 // What a call does and where it keeps it.
 struct Layout {
@@ -1057,7 +1062,7 @@ struct Layout {
     int a_terms, a16_terms, w16_terms, u_terms, u16_terms;
     int score_most, dA_most, dW_most;                  // pairs of terms
     Tiling scores, dA, dW;
-    size_t rows, label, g, exp_g, lse, loss, z_label, count, top, exp_a, exp_w, partial, acc, a, a16, w, z, u, u16, bytes;
+    size_t rows, label, g, exp_g, factor, lse, loss, z_label, count, top, exp_a, exp_w, partial, acc, a, a16, w, z, u, u16, bytes;
 };
 }  // namespace
 
@@ -1116,6 +1121,7 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     l.loss = take((size_t)l.n_padded * 4);
     l.z_label = take((size_t)l.n_padded * 4);
     l.count = take(4);
+    l.factor = take(4);
     l.top = take(4);
     if (l.f16) {
         l.exp_a = take((size_t)l.n_padded * 4);
@@ -1141,7 +1147,7 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
 // way to memory and back.  A score costs 2 D flops a pair of terms again, at about 1.1 PFLOP/s, or some 12 bytes at 4 TB/s.
 static bool keeps_scores(const XentCall& c, bool forward, bool grads) {
     const int64_t n = c.n > 0 ? c.n : 1, whole = up(c.J, 256);
-    if ((size_t)up(n, 256) * whole * 4 > kXePieceBytes) return false;
+    if ((size_t)up(n, 256) * whole * 4 > kXeScoreBytes) return false;
     const int pairs = c.a_bf16 && c.w_bf16 ? 1 : c.a_bf16 || c.w_bf16 ? 2 : 3;
     const int64_t tiles = ((c.J + 127) / 128) * ((n + 127) / 128);
     return n > 64 && c.D * pairs >= 1500 && ((forward && grads) || tiles < 200);
@@ -1205,6 +1211,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     int* const top = (int*)(ws + l.top);
     float* const g = (float*)(ws + l.g);
     int* const exp_g = (int*)(ws + l.exp_g);
+    float* const factor = (float*)(ws + l.factor);
     float* const lse = (float*)(ws + l.lse);
     float* const loss = (float*)(ws + l.loss);
     bf16_t* const A = (bf16_t*)(ws + l.a);
@@ -1222,7 +1229,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         p.a = c.a; p.lda = c.lda; p.n = (int)c.n; p.J = (int)c.J; p.D = (int)c.D; p.n_padded = (int)l.n_padded;
         p.y = c.y; p.weight = c.weight; p.scale = c.scale; p.mean = c.mean;
         p.rows = rows; p.label = label; p.exp_g = exp_g; p.count = count; p.g = g;
-        p.lse_packed = lse; p.lse_given = forward ? nullptr : c.lse;
+        p.lse_packed = lse; p.factor = factor; p.lse_given = forward ? nullptr : c.lse;
         p.to = A; p.ld = l.ld_a; p.plane = a_plane; p.terms = l.a_terms; p.window = l.window;
         p.to16 = A16; p.ld16 = l.f16 ? l.ld_k : 0; p.plane16 = a16_plane; p.terms16 = l.a16_terms; p.exps = exp_a;
         p.zero = grads ? c.dA : nullptr; p.ld_zero = c.ldda;
@@ -1332,11 +1339,11 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         const bool alone = n_some <= 64;
         hipLaunchKernelGGL(xent_loss_kernel, dim3(alone ? 1u : (uint32_t)((n_some + 15) / 16)), dim3(1024), 0, s, (const float2*)(ws + l.partial), tiles,
                            (int)l.ld_partial, (const int*)rows, (const int*)count, (const float*)(ws + l.z_label), (const float*)g, c.loss, c.lse, lse, loss,
-                           alone ? c.total : nullptr);
+                           (const float*)factor, alone ? c.total : nullptr);
         total_done = alone;
     }
     if (forward && c.total && !total_done)
-        hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, c.total);
+        hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, (const float*)factor, c.total);
     e = hipGetLastError();
     if (e != hipSuccess || !grads) return e;
 
@@ -1364,6 +1371,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             p.k_tiles = (int)((n + 63) / 64); p.last_y = 64 * (p.k_tiles - 1);
             p.pairs = l.f16 ? pair_list(l.w16_terms, l.u16_terms, l.dA_most, &p.pair_x, &p.pair_y) : 1;
             p.exp_n = exp_g; p.exp_top = top;
+            p.factor = factor;
             p.splits = l.dA.splits;
             p.count = count; p.n_is_rows = true;
             if (l.dA.splits == 1 && i == 0) {                            // the last sum goes straight to its row
@@ -1388,6 +1396,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             p.pairs = l.f16 ? pair_list(l.a_terms, l.u_terms, l.dW_most, &p.pair_x, &p.pair_y) : 1;
             p.splits = 1;
             p.count = count; p.k_is_rows = true;
+            p.factor = factor;
             p.ldo = c.lddw;
             if (c.w_bf16) {
                 p.out = (bf16_t*)c.dW + first * c.lddw;
