@@ -82,20 +82,30 @@ __device__ __forceinline__ uint32_t aw_code(float x, uint32_t r) {
 }
 __device__ __forceinline__ float aw_finite(float x) { return fabsf(x) < __builtin_inff() ? fabsf(x) : 0.f; }
 
-__device__ __forceinline__ float aw_first(uint32_t code) {               // sign, e4m3
-    const uint32_t mag = code & 0x7f;
-    float x = mag < 8 ? (float)mag * 0x1p-9f : __uint_as_float((mag << 20) + (120u << 23));
-    if (mag == 0x7f) x = __builtin_nanf("");
-    return code & 0x80 ? -x : x;
-}
 __device__ __forceinline__ float aw_second(uint32_t code) {
     return (float)__builtin_bit_cast(_Float16, (uint16_t)(code << 7));
 }
+// values of eight codes
+__device__ __forceinline__ void aw_firsts(uint2 c, float scale, float (&x)[8]) {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8(c.x, 0); x[1] = __builtin_amdgcn_cvt_f32_fp8(c.x, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8(c.x, 2); x[3] = __builtin_amdgcn_cvt_f32_fp8(c.x, 3);
+    x[4] = __builtin_amdgcn_cvt_f32_fp8(c.y, 0); x[5] = __builtin_amdgcn_cvt_f32_fp8(c.y, 1);
+    x[6] = __builtin_amdgcn_cvt_f32_fp8(c.y, 2); x[7] = __builtin_amdgcn_cvt_f32_fp8(c.y, 3);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= scale;
+}
+__device__ __forceinline__ void aw_seconds(uint2 c, float scale, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = aw_second((c.x >> (8 * e)) & 0xff) * scale;
+        x[4 + e] = aw_second((c.y >> (8 * e)) & 0xff) * scale;
+    }
+}
 
-// eight elements at any address; those at and beyond `left` read as 0
-template <class T, bool WIDE>
-__device__ __forceinline__ void aw_load(const T* p, int left, float (&x)[8]) {
-    if constexpr (WIDE) {
+// Eight elements: at once (`wide`), or one by one at any address, those at and beyond `left` read as 0 and not written
+template <class T>
+__device__ __forceinline__ void aw_load(const T* p, bool wide, int left, float (&x)[8]) {
+    if (wide) {
         if constexpr (sizeof(T) == 4) {
             const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll
@@ -113,17 +123,19 @@ __device__ __forceinline__ void aw_load(const T* p, int left, float (&x)[8]) {
         }
     }
 }
-template <bool WIDE>
-__device__ __forceinline__ uint64_t aw_codes(const uint8_t* p, int left) {
-    if constexpr (WIDE) return *reinterpret_cast<const uint64_t*>(p);
-    uint64_t x = 0;
+__device__ __forceinline__ uint2 aw_codes(const uint8_t* p, bool wide, int left) {
+    if (wide) return *reinterpret_cast<const uint2*>(p);
+    uint2 x = make_uint2(0u, 0u);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x |= e < left ? (uint64_t)p[e] << (8 * e) : 0ull;
+    for (int e = 0; e < 4; ++e) {
+        x.x |= e < left ? (uint32_t)p[e] << (8 * e) : 0u;
+        x.y |= 4 + e < left ? (uint32_t)p[4 + e] << (8 * e) : 0u;
+    }
     return x;
 }
-template <class T, bool WIDE>
-__device__ __forceinline__ void aw_store(T* p, int left, const float (&x)[8]) {
-    if constexpr (WIDE) {
+template <class T>
+__device__ __forceinline__ void aw_store(T* p, bool wide, int left, const float (&x)[8]) {
+    if (wide) {
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
             *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
@@ -139,78 +151,76 @@ __device__ __forceinline__ void aw_store(T* p, int left, const float (&x)[8]) {
             }
     }
 }
-template <bool WIDE>
-__device__ __forceinline__ void aw_store_codes(uint8_t* p, int left, uint64_t x) {
-    if constexpr (WIDE) {
-        *reinterpret_cast<uint64_t*>(p) = x;
+__device__ __forceinline__ void aw_store_codes(uint8_t* p, bool wide, int left, uint2 x) {
+    if (wide) {
+        *reinterpret_cast<uint2*>(p) = x;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) p[e] = (uint8_t)(x >> (8 * e));
+        for (int e = 0; e < 4; ++e) {
+            if (e < left) p[e] = (uint8_t)(x.x >> (8 * e));
+            if (4 + e < left) p[4 + e] = (uint8_t)(x.y >> (8 * e));
+        }
     }
 }
 
 struct AwNow {
-    float scale, lr, c1, c2;                                             // of the gradient, the rate, 1 - b1^t and 1 - b2^t
+    float scale, lr, by_c1, by_c2;                                       // of the gradient, the rate, 1 / (1 - b1^t) and 1 / (1 - b2^t)
     uint32_t key;
 };
 
-template <class G, int BITS, bool WIDE>
+// left < 8: the tensor ends among the thread's elements, or before them (left = 0; the thread goes along for its block's maximum)
+template <class G, int BITS, bool WHOLE>
 __device__ __forceinline__ void aw_elements(const AdamwTensor& t, const AdamwRates& r, const AwNow& now, int64_t at, int left) {
 #pragma clang fp contract(off)
+    const bool wide = WHOLE || (t.wide && left == 8);
     float p[8], g[8], m[8], v[8];
-    aw_load<G, WIDE>((const G*)t.g + at, left, g);
-    aw_load<float, WIDE>(t.p + at, left, p);
-    uint64_t mc = 0, vc = 0;
+    aw_load((const G*)t.g + at, wide, left, g);
+    aw_load(t.p + at, wide, left, p);
     if constexpr (BITS == 32) {
-        aw_load<float, WIDE>((const float*)t.m + at, left, m);
-        aw_load<float, WIDE>((const float*)t.v + at, left, v);
+        aw_load((const float*)t.m + at, wide, left, m);
+        aw_load((const float*)t.v + at, wide, left, v);
     } else {
-        mc = aw_codes<WIDE>((const uint8_t*)t.m + at, left);
-        vc = aw_codes<WIDE>((const uint8_t*)t.v + at, left);
-        const float ms = aw_pow2((int)t.m_scale[at >> 7] - 127), vs = aw_pow2((int)t.v_scale[at >> 7] - 127);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            m[e] = aw_first((uint32_t)(mc >> (8 * e)) & 0xff) * ms;
-            v[e] = aw_second((uint32_t)(vc >> (8 * e)) & 0xff) * vs;
-        }
+        const uint2 mc = aw_codes((const uint8_t*)t.m + at, wide, left), vc = aw_codes((const uint8_t*)t.v + at, wide, left);
+        aw_firsts(mc, aw_pow2((int)t.m_scale[at >> 7] - 127), m);
+        aw_seconds(vc, aw_pow2((int)t.v_scale[at >> 7] - 127), v);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float x = g[e] * now.scale;
         m[e] = m[e] * r.beta1 + x * r.one_beta1;
         v[e] = v[e] * r.beta2 + x * x * r.one_beta2;
-        const float move = (m[e] / now.c1) / (sqrtf(v[e] / now.c2) + r.eps);
+        // square root and reciprocal to one unit in the last place: p moves by lr of this, and is rounded itself
+        const float move = (m[e] * now.by_c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e] * now.by_c2) + r.eps);
         p[e] = p[e] - now.lr * (move + r.decay * p[e]);
     }
-    aw_store<float, WIDE>(t.p + at, left, p);
-    if (t.copy) aw_store<bf16_t, WIDE>((bf16_t*)t.copy + at, left, p);
+    aw_store(t.p + at, wide, left, p);
+    if (t.copy) aw_store((bf16_t*)t.copy + at, wide, left, p);
     if constexpr (BITS == 32) {
-        aw_store<float, WIDE>((float*)t.m + at, left, m);
-        aw_store<float, WIDE>((float*)t.v + at, left, v);
+        aw_store((float*)t.m + at, wide, left, m);
+        aw_store((float*)t.v + at, wide, left, v);
     } else {
         float top_m = 0.f, top_v = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            top_m = fmaxf(top_m, e < left ? aw_finite(m[e]) : 0.f);
-            top_v = fmaxf(top_v, e < left ? aw_finite(v[e]) : 0.f);
+            top_m = fmaxf(top_m, aw_finite(m[e]));                       // (elements that are not there are 0)
+            top_v = fmaxf(top_v, aw_finite(v[e]));
         }
         const int km = aw_scale<7>(aw_row_max(top_m)), kv = aw_scale<14>(aw_row_max(top_v));
         const float dm = aw_pow2(-km), dv = aw_pow2(-kv);
         const uint64_t number = (uint64_t)t.first * 128u + (uint64_t)at;
-        uint32_t key = now.key ^ ((uint32_t)(number >> 32) * 0x9E3779B9u);
-        uint64_t mo = 0, vo = 0;
+        const uint32_t key = now.key ^ ((uint32_t)(number >> 32) * 0x9E3779B9u);
+        uint32_t mo[2] = {0u, 0u}, vo[2] = {0u, 0u};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t h = aw_mix((uint32_t)(number + e) ^ key);
             const uint32_t a = aw_code<7, 0x7f>(fabsf(m[e]) * dm, h & 0xffffu) | (__float_as_uint(m[e]) >> 31 << 7);
             uint32_t b = aw_code<15, 0xff>(v[e] * dv, h >> 16);
             if (v[e] > 0.f) b = max(b, 1u);
-            mo |= (uint64_t)a << (8 * e);
-            vo |= (uint64_t)b << (8 * e);
+            mo[e / 4] |= a << (8 * (e % 4));
+            vo[e / 4] |= b << (8 * (e % 4));
         }
-        aw_store_codes<WIDE>((uint8_t*)t.m + at, left, mo);
-        aw_store_codes<WIDE>((uint8_t*)t.v + at, left, vo);
+        aw_store_codes((uint8_t*)t.m + at, wide, left, make_uint2(mo[0], mo[1]));
+        aw_store_codes((uint8_t*)t.v + at, wide, left, make_uint2(vo[0], vo[1]));
         if ((threadIdx.x & 15) == 0 && left > 0) {
             t.m_scale[at >> 7] = (uint8_t)(km + 127);
             t.v_scale[at >> 7] = (uint8_t)(kv + 127);
@@ -225,9 +235,9 @@ __global__ __launch_bounds__(kAwThreads) void adamw_kernel(const AdamwTable tabl
     if (now.scale != now.scale) return;                                  // a gradient that is not finite: no step
     const int step = *r.step + 1;
     now.lr = r.lr_scale ? r.lr * *r.lr_scale : r.lr;
-    // 1 - b^t; log b in 64 bits from the host
-    now.c1 = (float)-expm1((double)step * r.log_beta1);
-    now.c2 = (float)-expm1((double)step * r.log_beta2);
+    // 1 - b^t, log b in 64 bits from the host: the exponent's own rounding is 2^-24 of it, and so is that of the result at most
+    now.by_c1 = -1.f / expm1f((float)((double)step * r.log_beta1));
+    now.by_c2 = -1.f / expm1f((float)((double)step * r.log_beta2));
     now.key = aw_mix(r.seed + (uint32_t)step * 0x9E3779B9u);
     const int i = aw_tensor_of(table, blockIdx.x);
     const AdamwTensor t = table.t[i];
@@ -235,14 +245,13 @@ __global__ __launch_bounds__(kAwThreads) void adamw_kernel(const AdamwTable tabl
     if (t.wide && begin + kAwChunk <= t.n) {
 #pragma unroll
         for (int k = 0; k < kAwRounds; ++k) aw_elements<G, BITS, true>(t, r, now, begin + (k * kAwThreads + threadIdx.x) * kAwPer, 8);
-    } else {
+        return;
+    }
 #pragma unroll 1
-        for (int k = 0; k < kAwRounds; ++k) {
-            const int64_t at = begin + (k * kAwThreads + threadIdx.x) * kAwPer;
-            const int64_t left = t.n - at;
-            // threads behind the end go along (the block's maximum is over all 16 lanes), at the tensor's last element, storing nothing
-            aw_elements<G, BITS, false>(t, r, now, left > 0 ? at : ((t.n - 1) & ~(int64_t)7), left > 8 ? 8 : left > 0 ? (int)left : 0);
-        }
+    for (int k = 0; k < kAwRounds; ++k) {
+        const int64_t at = begin + (k * kAwThreads + threadIdx.x) * kAwPer, left = t.n - at;
+        // (a thread behind the end reads its block's scale at the tensor's last element)
+        aw_elements<G, BITS, false>(t, r, now, left > 0 ? at : ((t.n - 1) & ~(int64_t)7), left >= 8 ? 8 : left > 0 ? (int)left : 0);
     }
 }
 
@@ -256,27 +265,16 @@ __global__ __launch_bounds__(kAwThreads) void adamw_unpack_kernel(const AdamwTab
     const int i = aw_tensor_of(table, blockIdx.x);
     const AdamwTensor t = table.t[i];
     const int64_t begin = (int64_t)(blockIdx.x - table.first_chunk[i]) * kAwChunk;
-    const bool wide = t.wide && begin + kAwChunk <= t.n;
     for (int k = 0; k < kAwRounds; ++k) {
         const int64_t at = begin + (k * kAwThreads + threadIdx.x) * kAwPer;
         if (at >= t.n) return;
         const int left = t.n - at > 8 ? 8 : (int)(t.n - at);
-        const uint64_t mc = wide ? aw_codes<true>((const uint8_t*)t.m + at, 8) : aw_codes<false>((const uint8_t*)t.m + at, left);
-        const uint64_t vc = wide ? aw_codes<true>((const uint8_t*)t.v + at, 8) : aw_codes<false>((const uint8_t*)t.v + at, left);
-        const float ms = aw_pow2((int)t.m_scale[at >> 7] - 127), vs = aw_pow2((int)t.v_scale[at >> 7] - 127);
+        const bool wide = t.wide && left == 8;
         float m[8], v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            m[e] = aw_first((uint32_t)(mc >> (8 * e)) & 0xff) * ms;
-            v[e] = aw_second((uint32_t)(vc >> (8 * e)) & 0xff) * vs;
-        }
-        if (wide) {
-            aw_store<bf16_t, true>((bf16_t*)t.p + at, 8, m);             // (outputs travel in p and copy)
-            aw_store<bf16_t, true>((bf16_t*)t.copy + at, 8, v);
-        } else {
-            aw_store<bf16_t, false>((bf16_t*)t.p + at, left, m);
-            aw_store<bf16_t, false>((bf16_t*)t.copy + at, left, v);
-        }
+        aw_firsts(aw_codes((const uint8_t*)t.m + at, wide, left), aw_pow2((int)t.m_scale[at >> 7] - 127), m);
+        aw_seconds(aw_codes((const uint8_t*)t.v + at, wide, left), aw_pow2((int)t.v_scale[at >> 7] - 127), v);
+        aw_store((bf16_t*)t.p + at, wide, left, m);                      // (outputs travel in p and copy)
+        aw_store((bf16_t*)t.copy + at, wide, left, v);
     }
 }
 
@@ -334,7 +332,7 @@ hipError_t launch_adamw_unpack(const AdamwTensor* t, int count, hipStream_t s) {
 // ---------------------------------------------------------------------------------------------------------------
 // norm = sqrt(sum of all g^2) in 64 bits (squares of fp32 numbers overflow fp32; the units have 64-bit products to spare beside
 // the reads), added per workgroup, then by one workgroup in a fixed order.  factor = min(1, max_norm / norm), NaN if the norm is not finite.
-constexpr int kGnChunk = 16384;
+constexpr int kGnChunk = 8192;
 
 struct GradTable {
     GradTensor t[kGradTensors];
@@ -347,12 +345,16 @@ __device__ __forceinline__ double gn_wave_sum(double x) {
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
     return x;
 }
-__device__ __forceinline__ double gn_block_sum(double x) {               // four wavefronts; in thread 0
-    __shared__ double part[4];
+template <int WAVES>
+__device__ __forceinline__ double gn_block_sum(double x) {               // in thread 0
+    __shared__ double part[WAVES];
     x = gn_wave_sum(x);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    return (part[0] + part[1]) + (part[2] + part[3]);
+    x = part[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) x += part[w];
+    return x;
 }
 
 template <class G>
@@ -362,33 +364,38 @@ __global__ __launch_bounds__(kAwThreads) void grad_norm_kernel(const GradTable t
     const G* const g = (const G*)t.g;
     const int64_t begin = (int64_t)(blockIdx.x - table.first_chunk[i]) * kGnChunk;
     double s[8] = {};
-    if (t.wide && begin + kGnChunk <= t.n) {
+    auto add = [&](const float(&x)[8]) {
 #pragma unroll
-        for (int k = 0; k < kGnChunk / (kAwThreads * 8); ++k) {
-            float x[8];
-            aw_load<G, true>(g + begin + (k * kAwThreads + threadIdx.x) * 8, 8, x);
+        for (int e = 0; e < 8; ++e) s[e] = __builtin_fma((double)x[e], (double)x[e], s[e]);
+    };
+    constexpr int ROUNDS = kGnChunk / (kAwThreads * 8);
+    if (t.wide && begin + kGnChunk <= t.n) {                             // a whole chunk: all of it on its way at once
+        float x[ROUNDS][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] = __builtin_fma((double)x[e], (double)x[e], s[e]);
-        }
+        for (int k = 0; k < ROUNDS; ++k) aw_load(g + begin + (k * kAwThreads + threadIdx.x) * 8, true, 8, x[k]);
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) add(x[k]);
     } else {
-        for (int64_t at = begin + threadIdx.x; at < t.n && at < begin + kGnChunk; at += kAwThreads) {
-            float x;
-            if constexpr (sizeof(G) == 4) x = g[at];
-            else x = bf16_to_f32(g[at]);
-            s[0] = __builtin_fma((double)x, (double)x, s[0]);
+        for (int k = 0; k < ROUNDS; ++k) {
+            const int64_t at = begin + (k * kAwThreads + threadIdx.x) * 8, left = t.n - at;
+            if (left <= 0) break;
+            float x[8];
+            aw_load(g + at, t.wide && left >= 8, left >= 8 ? 8 : (int)left, x);
+            add(x);
         }
     }
-    const double sum = gn_block_sum(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
+    const double sum = gn_block_sum<kAwThreads / 64>(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(kAwThreads) void grad_norm_sum_kernel(const double* __restrict__ partial, int64_t n, float max_norm,
-                                                                   float* __restrict__ out) {
-    double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kAwThreads) s += partial[i];
-    s = gn_block_sum(s);
+__global__ __launch_bounds__(1024) void grad_norm_sum_kernel(const double* __restrict__ partial, int64_t n, float max_norm, float* __restrict__ out) {
+    double s[8] = {};
+    for (int64_t i = threadIdx.x; i < n; i += 8192)                      // eight on their way at a time
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += i + 1024 * k < n ? partial[i + 1024 * k] : 0.0;
+    const double sum = gn_block_sum<16>(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
     if (threadIdx.x == 0) {
-        const double norm = sqrt(s), f = (double)max_norm / norm;
+        const double norm = sqrt(sum), f = (double)max_norm / norm;
         out[0] = (float)norm;
         out[1] = !(norm < __builtin_inf()) ? __builtin_nanf("") : f < 1.0 ? (float)f : 1.f;
     }
@@ -423,7 +430,7 @@ hipError_t launch_grad_norm(const GradTensor* t, int count, bool bf16, float max
         if (e != hipSuccess) return e;
         before += chunks;
     }
-    hipLaunchKernelGGL(grad_norm_sum_kernel, dim3(1), dim3(kAwThreads), 0, s, (const double*)partial, before, max_norm, out);
+    hipLaunchKernelGGL(grad_norm_sum_kernel, dim3(1), dim3(1024), 0, s, (const double*)partial, before, max_norm, out);
     return hipGetLastError();
 }
 

@@ -24,6 +24,8 @@
 
 namespace sfb {
 
+typedef uint32_t xe_u32x4u __attribute__((ext_vector_type(4), aligned(2)));   // a 16-byte access at any bf16's address
+
 constexpr int kXeK = 64;           // k of a stage: 128 bytes of a row
 enum XentEnd { kXeStats = 0, kXeU = 1, kXeStore = 2 };
 
@@ -58,7 +60,6 @@ struct XentProduct {
     const float* add;                        // fp32, or nullptr
     int64_t ld_add;
     const int* row_map;                      // row of out for n, or nullptr
-    bool wide;                               // out takes 16 bytes at a time
 };
 
 __device__ __forceinline__ uint32_t xe_lds_address(const void* p) {
@@ -482,12 +483,12 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
                     hi += *reinterpret_cast<const f32x4*>(p + 4);
                 }
                 Out* const o = out + (int64_t)(a.row_map ? a.row_map[n] : n) * a.ldo + m;
-                if (a.wide && m + 8 <= a.M) {
+                if (m + 8 <= a.M) {                                      // (at the elements' own alignment)
                     if constexpr (sizeof(Out) == 4) {
-                        *reinterpret_cast<f32x4*>(o) = lo;
-                        *reinterpret_cast<f32x4*>(o + 4) = hi;
+                        *reinterpret_cast<sp_f32x4u*>(o) = lo;
+                        *reinterpret_cast<sp_f32x4u*>(o + 4) = hi;
                     } else {
-                        *reinterpret_cast<sp_u32x4*>(o) = sp_u32x4{cvt_pk_bf16(lo[0], lo[1]), cvt_pk_bf16(lo[2], lo[3]), cvt_pk_bf16(hi[0], hi[1]), cvt_pk_bf16(hi[2], hi[3])};
+                        *reinterpret_cast<xe_u32x4u*>(o) = xe_u32x4u{cvt_pk_bf16(lo[0], lo[1]), cvt_pk_bf16(lo[2], lo[3]), cvt_pk_bf16(hi[0], hi[1]), cvt_pk_bf16(hi[2], hi[3])};
                     }
                 } else {
 #pragma unroll
@@ -600,39 +601,42 @@ __device__ __forceinline__ float xe_top4(f32x4 x, float top) {
 }
 __device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float_as_uint(top) >> 23) - 127 - 14; }   // (2^-126 for all below)
 
-// A row of D elements by a workgroup of 256: the first 4096 stay in registers between what looks them over and what takes them.
-template <class T>
+// A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 1024): the first 16 a thread stay
+// in registers between what looks them over and what takes them.
+template <class T, int LANES>
 struct XentRow {
     f32x4 held[4];
     const T* row;
-    int D;
-    __device__ __forceinline__ XentRow(const T* r, int d) : row(r), D(d) {
+    int D, lane;
+    __device__ __forceinline__ XentRow(const T* r, int d) : row(r), D(d), lane(threadIdx.x & (LANES - 1)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) held[i] = load4(row, (int)threadIdx.x * 4 + 1024 * i, D);
+        for (int i = 0; i < 4; ++i) held[i] = load4(row, lane * 4 + 4 * LANES * i, D);
     }
     // f(d, four elements from d on), d < whole; zeros from D on
     template <class F>
     __device__ __forceinline__ void each(int64_t whole, F f) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int d = (int)threadIdx.x * 4 + 1024 * i;
+            const int d = lane * 4 + 4 * LANES * i;
             if (d < whole) f(d, held[i]);
         }
 #pragma unroll 4
-        for (int d = (int)threadIdx.x * 4 + 4096; d < whole; d += 1024) f(d, load4(row, d, D));
+        for (int d = lane * 4 + 16 * LANES; d < whole; d += 4 * LANES) f(d, load4(row, d, D));
     }
     // exponent that brings the largest finite magnitude into [2^14, 2^15) (2^-126 for all below)
     __device__ __forceinline__ int exponent() const {
-        __shared__ float part[4];
         float top = 0.f;
         each(D, [&](int, f32x4 x) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.f);
         });
         top = wave_max(top);
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        if constexpr (LANES == 256) {
+            __shared__ float part[4];
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        }
         return (int)(__float_as_uint(top) >> 23) - 127 - 14;
     }
 };
@@ -673,7 +677,7 @@ __device__ __forceinline__ void xe_pack_row(const XentPack& p, int k) {
         return;
     }
     const T* const src = (const T*)p.a + (int64_t)i * p.lda;
-    const XentRow<T> row(src, p.D);
+    const XentRow<T, 256> row(src, p.D);
     int e0 = 0;
     if (p.terms16) {
         e0 = row.exponent();
@@ -701,40 +705,50 @@ struct XentWords {
     int* exps;
 };
 // Row k of W's piece in one bf16 term or (F16) fp16 terms and its exponent; zeros to whole stages and for rows from n on.
-template <class T, bool F16>
+template <class T, bool F16, int LANES>
 __device__ __forceinline__ void xe_pack_word(const XentWords& p, int k) {
     bf16_t* const out = p.to + (int64_t)k * p.ldd;
+    const int lane = threadIdx.x & (LANES - 1);
     if (k >= p.n) {
-        for (int d = threadIdx.x * 4; d < p.ldd; d += 1024) xe_put(out + d, p.plane, p.terms, f32x4{0.f, 0.f, 0.f, 0.f});
-        if (F16 && threadIdx.x == 0) p.exps[k] = -200;                   // below any other: has no say in the largest
+        for (int d = lane * 4; d < p.ldd; d += 4 * LANES) xe_put(out + d, p.plane, p.terms, f32x4{0.f, 0.f, 0.f, 0.f});
+        if (F16 && lane == 0) p.exps[k] = -200;                          // below any other: has no say in the largest
         return;
     }
-    const XentRow<T> row((const T*)p.w + (int64_t)k * p.ld, p.D);
+    const XentRow<T, LANES> row((const T*)p.w + (int64_t)k * p.ld, p.D);
     if constexpr (F16) {
         const int e0 = row.exponent();
-        if (threadIdx.x == 0) p.exps[k] = e0;
+        if (lane == 0) p.exps[k] = e0;
         row.each(p.ldd, [&](int d, f32x4 v) { xe_put16(out + d, p.plane, p.terms, v, e0); });
     } else {
         row.each(p.ldd, [&](int d, f32x4 v) { xe_put(out + d, p.plane, 1, v); });
     }
 }
+// Workgroup b's rows: four short ones (a wavefront each) or one.  The rows are padded to whole multiples of 64.
+constexpr int kXeShortRow = 1024;
+template <class T, bool F16>
+__device__ __forceinline__ void xe_pack_words(const XentWords& p, int b) {
+    if (p.D <= kXeShortRow) xe_pack_word<T, F16, 64>(p, 4 * b + (threadIdx.x >> 6));
+    else xe_pack_word<T, F16, 256>(p, b);
+}
 
 template <class T>
 __global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) { xe_pack_row<T>(p, blockIdx.x); }
 template <class T, bool F16>
-__global__ __launch_bounds__(256) void xent_pack_words_kernel(const XentWords w) { xe_pack_word<T, F16>(w, blockIdx.x); }
+__global__ __launch_bounds__(256) void xent_pack_words_kernel(const XentWords w) { xe_pack_words<T, F16>(w, blockIdx.x); }
 // The rows and the first piece's words in one launch
 template <class TA, class TW, bool F16>
 __global__ __launch_bounds__(256) void xent_pack_both_kernel(const XentPack p, const XentWords w) {
     if ((int)blockIdx.x < p.n_padded) xe_pack_row<TA>(p, blockIdx.x);
-    else xe_pack_word<TW, F16>(w, (int)blockIdx.x - p.n_padded);
+    else xe_pack_words<TW, F16>(w, (int)blockIdx.x - p.n_padded);
 }
 
 // The largest of a piece's exponents
 __global__ __launch_bounds__(1024) void xent_top_kernel(const int* __restrict__ exps, int n, int* __restrict__ top) {
     __shared__ int part[16];
     int m = -200;
-    for (int i = threadIdx.x; i < n; i += 1024) m = max(m, exps[i]);
+    for (int i = threadIdx.x; i < n; i += 8192)                          // eight on their way at a time
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = max(m, exps[min(i + 1024 * k, n - 1)]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o, kWave));
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
@@ -933,7 +947,15 @@ __global__ __launch_bounds__(256) void xent_rows_out_kernel(const float* __restr
     const int k = (int)(c / per), d = (int)(c % per) * 4;
     if (k >= *count) return;
     f32x4 s{0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < planes; ++p) s += *reinterpret_cast<const f32x4*>(acc + p * plane + (int64_t)k * ld + d);
+    const float* const at = acc + (int64_t)k * ld + d;
+    for (int p = 0; p < planes; p += 8) {                                // eight on their way at a time
+        f32x4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4*>(at + min(p + i, planes - 1) * plane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (p + i < planes) s += x[i];
+    }
     store4(out + (int64_t)rows[k] * ldo, d, D, s);
 }
 
@@ -1249,20 +1271,20 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             there = 0;
             return rows_too ? hipGetLastError() : hipSuccess;
         }
-        const int64_t padded = up(n, 64);
+        const int64_t padded = up(n, 64), groups = c.D <= kXeShortRow ? padded / 4 : padded;
         *w = Words{Wp, l.ld_k, w_plane, (int)padded};
         if (there == first) return hipSuccess;
         there = first;
         const XentWords x{(const char*)c.W + (size_t)first * c.ldw * (c.w_bf16 ? 2 : 4), c.ldw, (int)c.D, (int)n, Wp, l.ld_k, w_plane, l.f16 ? l.w16_terms : 1,
                           l.f16 ? exp_w + first : nullptr};
         if (rows_too) {
-            const dim3 grid((uint32_t)(l.n_padded + padded)), block(256);
+            const dim3 grid((uint32_t)(l.n_padded + groups)), block(256);
             if (!l.f16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, bf16_t, false>), grid, block, 0, s, pack, x);
             else if (c.w_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<float, bf16_t, true>), grid, block, 0, s, pack, x);
             else if (c.a_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, float, true>), grid, block, 0, s, pack, x);
             else hipLaunchKernelGGL((xent_pack_both_kernel<float, float, true>), grid, block, 0, s, pack, x);
         } else {
-            const dim3 grid((uint32_t)padded), block(256);
+            const dim3 grid((uint32_t)groups), block(256);
             if (!l.f16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, false>), grid, block, 0, s, x);
             else if (c.w_bf16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true>), grid, block, 0, s, x);
             else hipLaunchKernelGGL((xent_pack_words_kernel<float, true>), grid, block, 0, s, x);
@@ -1315,7 +1337,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             scores_of(first, n, w);
             XentProduct p = scores;
             p.splits = l.scores.splits;
-            p.out = (float*)(ws + l.z) + first; p.ldo = l.ld_z; p.out_plane = l.n_padded * l.ld_z; p.wide = true;
+            p.out = (float*)(ws + l.z) + first; p.ldo = l.ld_z; p.out_plane = l.n_padded * l.ld_z;
             e = l.f16 ? launch_product<false, false, true, kXeStore, float>(p, l.scores.tile, s) : launch_product<false, false, false, kXeStore, float>(p, l.scores.tile, s);
             if (e != hipSuccess) return e;
         }
@@ -1376,9 +1398,8 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             p.count = count; p.n_is_rows = true;
             if (l.dA.splits == 1 && i == 0) {                            // the last sum goes straight to its row
                 p.out = c.dA; p.ldo = c.ldda; p.row_map = rows;
-                p.wide = c.ldda % 8 == 0 && ((uintptr_t)c.dA % 16) == 0;
             } else {
-                p.out = ws + l.acc; p.ldo = l.ld_acc; p.out_plane = acc_plane; p.wide = true;
+                p.out = ws + l.acc; p.ldo = l.ld_acc; p.out_plane = acc_plane;
             }
             p.add = i < pieces - 1 ? (const float*)(ws + l.acc) : nullptr; p.ld_add = l.ld_acc;
             if (p.row_map && c.a_bf16)
@@ -1400,11 +1421,9 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             p.ldo = c.lddw;
             if (c.w_bf16) {
                 p.out = (bf16_t*)c.dW + first * c.lddw;
-                p.wide = c.lddw % 8 == 0 && ((uintptr_t)c.dW % 16) == 0;
                 e = launch_product<true, true, false, kXeStore, bf16_t>(p, l.dW.tile, s);
             } else {
                 p.out = (float*)c.dW + first * c.lddw;
-                p.wide = c.lddw % 4 == 0 && ((uintptr_t)c.dW % 16) == 0;
                 e = launch_product<true, true, false, kXeStore, float>(p, l.dW.tile, s);
             }
             if (e != hipSuccess) return e;
