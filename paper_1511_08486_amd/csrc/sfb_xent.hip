@@ -70,13 +70,8 @@ __device__ __forceinline__ void xe_dma(const void* base, uint32_t off, uint32_t 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 
-// exp(x) with x's whole part taken off in two products, so that its error is that of exp2 of a number below 1/2; NaN stays
-__device__ __forceinline__ float xe_exp(float x) {
-    x = x < -104.f ? -104.f : x;
-    const float n = rintf(x * 1.44269504f);
-    const float r = __builtin_fmaf(x, 1.44269504f, -n) + x * 1.92596299e-8f;
-    return __builtin_ldexpf(__builtin_amdgcn_exp2f(r), (int)n);
-}
+// exp(x), x <= 0 or little more, off by |x| 2^-23 of itself: what x's own rounding, of a difference of two scores, is worth as well
+__device__ __forceinline__ float xe_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // How one operand goes to LDS and comes from there.  ROWS: of m (n) in the tile.  Not TR: LDS rows of 64 k, 16-byte piece p of row r at
 // p ^ (r & 7) ^ (r >> 3 & 1): sixteen consecutive rows on sixteen different bank groups (without the last bit half of all reads waited).  TR: LDS rows of ROWS m, 32-byte piece p of k-row r at p ^ turn(r), so that the four rows of a transposing read, and its
@@ -229,6 +224,17 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
+    // Tiles for few rows, whose vector units have time, add up blocks of 256 k: a score of 2048 k is rounded 16 times at an eighth of its
+    // size and 8 times at its whole, not 128 times (a single token's loss of 0.05 at scores of 20 was 6.1e-6 off, 6.5e-7 so)
+    constexpr bool BLOCKS = BN <= 64;
+    f32x16 sum[BLOCKS ? MT : 1][BLOCKS ? NT : 1];
+    if constexpr (BLOCKS) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sum[i][j] = acc[i][j];
+    }
+
     struct Frag { sp_u32x4 x[MT], y[NT]; };
     Frag f0, f1;
     auto read = [&](auto sc, auto rc, Frag& f, const unsigned char* lds) {
@@ -275,15 +281,29 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
         phase(I1, I1, I0, I0, f0, f1, now);
         phase(I2, I1, I0, I0, f1, f0, now);
         phase(I3, I1, I0, I0, f0, f1, now);
-        // behind the last product of a second term
         const int shrink_at = F16 && a.pairs > 1 ? (k_end - k_begin) * (a.pairs - 1) - 1 : -1;
-        auto shrink = [&](int s) {
-            if constexpr (F16) {
-                if (s == shrink_at) {
+        auto settle = [&](int s) {
+            if constexpr (BLOCKS) {
+                if ((s & 3) == 3) {
 #pragma unroll
                     for (int i = 0; i < MT; ++i)
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) acc[i][j] *= 1.f / 2048.f;
+                        for (int j = 0; j < NT; ++j) {
+                            sum[i][j] += acc[i][j];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+                        }
+                }
+            }
+            if constexpr (F16) {
+                if (s == shrink_at) {                                    // behind the last product of a second term
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) {
+                            acc[i][j] *= 1.f / 2048.f;
+                            if constexpr (BLOCKS) sum[i][j] *= 1.f / 2048.f;
+                        }
                 }
             }
         };
@@ -294,7 +314,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
             follow();
             aim();
             phase(I0, I1, I0, MID, f1, f0, now);
-            shrink(s);
+            settle(s);
             phase(I1, I1, MID, ALL, f0, f1, now);
             next();
             phase(I2, I1, I0, I0, f1, f0, now);
@@ -304,7 +324,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
             xe_wait_barrier();
             follow();
             phase(I0, I1, I0, I0, f1, f0, now);
-            shrink(s);
+            settle(s);
             phase(I1, I1, I0, I0, f0, f1, now);
             phase(I2, I1, I0, I0, f1, f0, now);
             phase(I3, I1, I0, I0, f0, f1, now);
@@ -312,6 +332,12 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
         phase(I0, I0, I0, I0, f1, f0, now);
     }
     xe_wait_barrier();                                                   // LDS is free
+    if constexpr (BLOCKS) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] += sum[i][j];
+    }
 
     const int mw = m0 + wm * MT * 32 + 4 * half, nw = n0 + wn * NT * 32 + l32;      // entry e of (i, j): m = mw + 32 i + 8 (e / 4) + e % 4
     // exponents of four m from mw + 32 i + 8 q on (the arrays reach to the end of the last tile)
