@@ -25,7 +25,8 @@ def hipcc():
 
 def build(verbose=False, extra_flags=()):
     """Compile every kernel translation unit and link libsfb.so next to this file."""
-    cmd = [hipcc(), *FLAGS, *extra_flags, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB]
+    jobs = max(1, min(8, os.cpu_count() or 1))          # translation units side by side
+    cmd = [hipcc(), *FLAGS, f"-parallel-jobs={jobs}", *extra_flags, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True, cwd=CSRC)
