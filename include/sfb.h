@@ -315,8 +315,8 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
  *               speeds it up (pieces of some 512 MB).  grads != 0: of the calls that form gradients.
  * sfb_xent_gradients and sfb_xent_loss_and_gradients give the same gradients, to rounding.  Results do not depend on the order in which
  * anything runs.  No two of the arrays may overlap.
- * SFB_EINVAL: a null pointer that is needed, a scale that is not finite, ws not aligned; SFB_ESHAPE: a leading dimension shorter than a row, n outside
- * [0, P*B]; SFB_EDTYPE; SFB_EUNSUPPORTED: not an SFB_MLR context, D beyond 2^22; SFB_EWORKSPACE.  Nothing is launched if an argument is refused.
+ * SFB_EINVAL: a null pointer that is needed or one not aligned to its type (ws: 256), a scale that is not finite; SFB_ESHAPE: a leading dimension shorter than a row, n outside
+ * [0, P*B]; SFB_EDTYPE; SFB_EUNSUPPORTED: not an SFB_MLR context, D or P*B beyond 2^22; SFB_EWORKSPACE.  Nothing is launched if an argument is refused.
  * Timed under family 8 (the first product of a call).
  */
 typedef struct sfb_xent {
@@ -362,7 +362,7 @@ SFB_API sfb_status sfb_xent_loss_and_gradients(sfb_ctx *ctx, const sfb_xent *x);
  *               step and the element's number; the same call on the same state gives the same bits.  All bytes 0 is a state of zeros.
  *               A moment above 0 of v keeps the smallest code; NaN and infinities become NaN and have no part in the scale.
  * Tensors are dense, at any alignment of their type (16 bytes, and 8 for codes, take wide accesses); none may overlap another.
- * n = 0 is skipped.  SFB_EINVAL: a null pointer that is needed, count < 0, a rate that is not finite or negative, a beta outside [0, 1), state_bits
+ * n = 0 is skipped.  SFB_EINVAL: a null pointer that is needed or one not aligned to its type, count < 0, a rate that is not finite or negative, a beta outside [0, 1), state_bits
  * neither 32 nor 8; SFB_ESHAPE: n < 0 or beyond 2^40; SFB_EDTYPE.  Nothing is launched if an argument is refused.
  * Timed under family 7.
  */

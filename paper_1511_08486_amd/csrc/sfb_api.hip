@@ -1049,10 +1049,13 @@ static bool aligned(const void* p, size_t to) { return ((uintptr_t)p % to) == 0;
 
 // ---- softmax cross entropy of a head -----------------------------------------------------------------------------
 
+// features and rows that 32-bit offsets and tile counts reach
+static bool xent_supported(const sfb_ctx* c) { return c->model == SFB_MLR && c->D <= (1 << 22) && (int64_t)c->P * c->B <= (1 << 22); }
+
 sfb_status sfb_xent_workspace_bytes(const sfb_ctx* c, sfb_dtype w_dtype, int32_t grads, size_t* least, size_t* best) {
     if (!c || (!least && !best)) return SFB_EINVAL;
     if (w_dtype != SFB_F32 && w_dtype != SFB_BF16) return SFB_EDTYPE;
-    if (c->model != SFB_MLR || c->D > (1 << 22)) return SFB_EUNSUPPORTED;
+    if (!xent_supported(c)) return SFB_EUNSUPPORTED;
     XentCall x{};
     x.w_bf16 = w_dtype == SFB_BF16; x.a_bf16 = c->dtype == SFB_BF16;
     x.n = (int64_t)c->P * c->B; x.J = c->J; x.D = c->D;
@@ -1064,12 +1067,14 @@ sfb_status sfb_xent_workspace_bytes(const sfb_ctx* c, sfb_dtype w_dtype, int32_t
 static sfb_status run_xent(sfb_ctx* c, const sfb_xent* x, bool forward, bool grads) {
     if (!c || !x || !x->W || !std::isfinite(x->scale)) return SFB_EINVAL;
     if (x->w_dtype != SFB_F32 && x->w_dtype != SFB_BF16) return SFB_EDTYPE;
-    if (c->model != SFB_MLR || c->D > (1 << 22)) return SFB_EUNSUPPORTED;
+    if (!xent_supported(c)) return SFB_EUNSUPPORTED;
     if (x->n < 0 || x->n > (int64_t)c->P * c->B) return SFB_ESHAPE;
     if (x->n > 0 && (!x->a || !x->y || (!forward && !x->lse))) return SFB_EINVAL;
     if (x->ldw < c->D || (x->n > 0 && x->lda < c->D)) return SFB_ESHAPE;
     const size_t wsz = x->w_dtype == SFB_BF16 ? 2 : 4, asz = c->dtype == SFB_BF16 ? 2 : 4;
     if (!aligned(x->W, wsz) || !aligned(x->a, asz)) return SFB_EINVAL;
+    for (const void* p : {(const void*)x->y, (const void*)x->loss, (const void*)x->lse, (const void*)x->total, (const void*)x->weight})
+        if (!aligned(p, 4)) return SFB_EINVAL;
     if (grads) {
         if (x->dA && (x->ldda < c->D)) return SFB_ESHAPE;
         if (x->dW && (x->lddw < c->D)) return SFB_ESHAPE;
@@ -1106,6 +1111,7 @@ static constexpr int64_t kMostElements = 1LL << 40;
 
 sfb_status sfb_adamw_step(sfb_ctx* c, const sfb_adamw_tensor* tensors, int32_t count, const sfb_adamw* o) {
     if (!c || !o || count < 0 || (count > 0 && !tensors) || !o->step) return SFB_EINVAL;
+    if (!aligned(o->step, 4) || !aligned(o->grad_scale, 4) || !aligned(o->lr_scale, 4)) return SFB_EINVAL;
     if (o->grad_dtype != SFB_F32 && o->grad_dtype != SFB_BF16) return SFB_EDTYPE;
     if (o->state_bits != 32 && o->state_bits != 8) return SFB_EINVAL;
     for (const float x : {o->lr, o->eps, o->weight_decay})
@@ -1191,7 +1197,7 @@ sfb_status sfb_grad_norm_bytes(const sfb_gradient* grads, int32_t count, size_t*
 
 sfb_status sfb_grad_norm(sfb_ctx* c, const sfb_gradient* grads, int32_t count, sfb_dtype grad_dtype, float max_norm, float* out, void* ws,
                          size_t ws_bytes) {
-    if (!c || !out || !(max_norm > 0.f)) return SFB_EINVAL;
+    if (!c || !out || !aligned(out, 4) || !(max_norm > 0.f)) return SFB_EINVAL;
     if (grad_dtype != SFB_F32 && grad_dtype != SFB_BF16) return SFB_EDTYPE;
     std::vector<GradTensor> list;
     sfb_status s = grad_list(grads, count, grad_dtype == SFB_BF16 ? 2 : 4, &list);

@@ -16,7 +16,8 @@ class SoftmaxHead(_Stream):
     """A head of J words on D features for up to `rows` rows a call, features in `dtype`, W in `w_dtype` ("f32" or "bf16").
     Owns an sfb_ctx and a workspace (workspace_bytes: as many, at least what the calls need; default: as many as speed them up).
     Rows whose label is outside [0, J) take no part.  Gradients come in the types of the features and of W; give one or both.
-    `gradients` reads the lse that `loss` left; `loss_and_gradients` is both in one call."""
+    `gradients` reads the lse that `loss` left; `loss_and_gradients` is both in one call.  Calls that may overlap in time, replays of
+    captured ones included, need a head each (it holds a workspace)."""
 
     def __init__(self, J, D, rows, dtype="bf16", w_dtype="bf16", workspace_bytes=None, gradients=True, stream=None, device="cuda:0"):
         self._a, self._w = _DTYPES[dtype], _DTYPES[w_dtype]
@@ -26,7 +27,7 @@ class SoftmaxHead(_Stream):
         self._check(lib.sfb_xent_workspace_bytes(self._ctx, self._w[0], 1 if gradients else 0, C.byref(least), C.byref(best)),
                     "sfb_xent_workspace_bytes")
         self.least_bytes, self.best_bytes = least.value, best.value
-        self._ws = torch.empty(self.best_bytes if workspace_bytes is None else int(workspace_bytes), dtype=torch.uint8, device=self.device)
+        self._ws = self._scratch(self.best_bytes if workspace_bytes is None else workspace_bytes)
 
     def _matrix(self, t, what, rows, dtype):
         if t is None:

@@ -14,12 +14,21 @@ class _Stream:
 
     def __init__(self, stream, device, shape=(SFB_MLR, 1, 1, 1, 1, SFB_F32)):
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
         if stream is None:
             stream = torch.cuda.current_stream(self.device).cuda_stream
         self.stream = int(stream)
         self._ctx = C.c_void_p()
         with torch.cuda.device(self.device):
             self._check(lib.sfb_create(C.byref(self._ctx), *shape, C.c_void_p(self.stream)), "sfb_create")
+
+    def _scratch(self, nbytes):
+        """A workspace that the allocator hands to nobody else before this stream is through with it."""
+        ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
+        if self.stream != torch.cuda.current_stream(self.device).cuda_stream:
+            ws.record_stream(torch.cuda.ExternalStream(self.stream, device=self.device))
+        return ws
 
     def _check(self, status, where):
         if status != 0:
@@ -67,7 +76,8 @@ _GRADS = (torch.float32, torch.bfloat16)
 class GradNorm(_Stream):
     """The norm of `grads` (fp32 or bf16, all of one type) as one vector, and the factor that clips it:
     out[0] = norm, out[1] = min(1, max_norm / norm), NaN if the norm is not finite.  Both stay on the device; hand out[1:] to
-    AdamW.step as grad_scale.  The gradients' memory is that of the construction; `grads` are kept alive with the object."""
+    AdamW.step as grad_scale.  The gradients' memory is that of the construction; `grads` are kept alive with the object.  Calls that may
+    overlap in time, replays of captured ones included, need an object each (it holds a workspace)."""
 
     def __init__(self, grads, stream=None, device="cuda:0"):
         super().__init__(stream, device)
@@ -75,7 +85,7 @@ class GradNorm(_Stream):
         self._list = (sfb_gradient * max(1, len(self.grads)))(*[sfb_gradient(t.data_ptr(), t.numel()) for t in self.grads])
         need = C.c_size_t()
         self._check(lib.sfb_grad_norm_bytes(self._list, len(self.grads), C.byref(need)), "sfb_grad_norm_bytes")
-        self._ws = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        self._ws = self._scratch(need.value)
         self._dtype = SFB_BF16 if self.grads and self.grads[0].dtype == torch.bfloat16 else SFB_F32
 
     def __call__(self, max_norm, out):
@@ -89,7 +99,7 @@ class AdamW(_Stream):
     """AdamW over lists of tensors: params fp32, grads fp32 or bf16, first and second moments fp32 or, with m_scales and v_scales
     (uint8, one for every 128 elements), uint8 codes; copies: bf16 tensors that receive the rounded parameters, or None.
     `step` is a device int32 that holds the steps taken (0 at first) and goes on counting in a replayed graph.  8-bit moments start
-    as zeros.  All tensors are kept alive with the object and keep their memory; step(grads=...) takes others for that call."""
+    as zeros.  All tensors are kept alive with the object and keep their memory; step(grads=...) takes others from then on."""
 
     def __init__(self, params, grads, m, v, step, m_scales=None, v_scales=None, copies=None, stream=None, device="cuda:0"):
         super().__init__(stream, device)

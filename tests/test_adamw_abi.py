@@ -33,6 +33,7 @@ def test_adamw_refuses(call):
         assert step(**{name: -1.0}) == -1 and step(**{name: float("nan")}) == -1 and step(**{name: float("inf")}) == -1
     for name in ("beta1", "beta2"):
         assert step(**{name: 1.0}) == -1 and step(**{name: -0.1}) == -1 and step(**{name: float("nan")}) == -1
+    assert step(step=P + 2) == -1 and step(grad_scale=P + 1) == -1 and step(lr_scale=P + 2) == -1
     assert step(state_bits=16) == -1 and step(grad_dtype=7) == -3
     for name in ("p", "g", "m", "v"):
         assert step(tensor={name: None}) == -1

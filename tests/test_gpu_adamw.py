@@ -336,3 +336,30 @@ def test_lists_that_do_not_fit_are_refused():
             opt.step(**bad)
     opt.sync()
     assert int(x["step"]) == 3
+
+
+def test_elements_beyond_32_bit_offsets():
+    """One tensor of 2^31 + 5000 elements, its norm and its step: the formulas at both ends."""
+    import paper_1511_08486_amd as sfb
+    n = (1 << 31) + 5000
+    p, m, v = (torch.zeros(n, device=DEV) for _ in range(3))
+    g = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    p.add_(0.5)
+    ends = [slice(0, 3000), slice(n - 3000, n)]
+    for e in ends:
+        g[e].normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    step, out = torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(2, device=DEV)
+    sfb.GradNorm([g])(1.0, out)
+    opt = sfb.AdamW([p], [g], [m], [v], step)
+    opt.step(**HYPER, grad_scale=out[1:])
+    opt.sync()
+    want = math.sqrt(sum(float((g[e].double() ** 2).sum()) for e in ends))
+    assert abs(float(out[0]) - want) <= 2 * EPS32 * want
+    for e in ends:
+        x = g[e].double().cpu().numpy()
+        w, wm, wv, _ = _formula(np.full(3000, 0.5), x, 0.0 * x, 0.0 * x, 1, scale=float(out[1]), **HYPER)
+        _close(p[e].double().cpu().numpy(), w, 4 * EPS32 + HYPER["lr"] * 16 * EPS32 + 0 * w, "p")
+        _close(m[e].double().cpu().numpy(), wm, 4 * EPS32 * np.abs(wm) + 1e-44, "m")
+        _close(v[e].double().cpu().numpy(), wv, 6 * EPS32 * wv + 1e-44, "v")
+    middle = p[n // 2:n // 2 + 1000]
+    assert torch.allclose(middle, torch.full_like(middle, 0.5 * (1 - HYPER["lr"] * HYPER["weight_decay"])), rtol=1e-6)

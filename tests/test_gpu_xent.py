@@ -366,3 +366,53 @@ def test_refusals():
     with pytest.raises(sfb.SfbError):
         small.loss_and_gradients(W, a, y, dA=dA, dW=dW)
     head.sync()
+
+
+def test_heads_on_streams_of_their_own():
+    """Two heads at once on two streams, each with its workspace, give what they give one after the other; "cuda" names the current GPU."""
+    import paper_1511_08486_amd as sfb
+    W, a, y = _inputs(300, 4000, 512, "bf16", "bf16", 40, padded=0.1)
+    W2, a2, y2 = _inputs(200, 3000, 640, "f32", "f32", 41)
+
+    def outs(n, J, D, t):
+        return dict(lse=torch.zeros(n, device=DEV), dA=torch.zeros(n, D, dtype=t, device=DEV), dW=torch.zeros(J, D, dtype=t, device=DEV))
+    sides = [torch.cuda.Stream(device=DEV) for _ in range(2)]
+    heads = [sfb.SoftmaxHead(4000, 512, 300, stream=sides[0].cuda_stream, device="cuda"),
+             sfb.SoftmaxHead(3000, 640, 200, dtype="f32", w_dtype="f32", stream=sides[1].cuda_stream, device="cuda")]
+    want, got = [[outs(300, 4000, 512, torch.bfloat16), outs(200, 3000, 640, torch.float32)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for h, o, x in zip(heads, want, ((W, a, y), (W2, a2, y2))):
+        h.loss_and_gradients(*x, **o)
+        h.sync()
+    for _ in range(3):
+        for h, o, x in zip(heads, got, ((W, a, y), (W2, a2, y2))):
+            h.loss_and_gradients(*x, **o)
+    torch.cuda.synchronize()
+    for o, w in zip(got, want):
+        assert all(torch.equal(o[k], w[k]) for k in o)
+
+
+def test_words_beyond_32_bit_offsets():
+    """W of 2.2e9 entries: the rows at its end, as words, labels and gradients."""
+    import paper_1511_08486_amd as sfb
+    n, J, D = 40, 140000, 16000
+    W = torch.empty(J, D, dtype=torch.bfloat16, device=DEV)
+    W.normal_(0.0, 0.02, generator=torch.Generator(device=DEV).manual_seed(3))
+    a = torch.randn(n, D, generator=torch.Generator().manual_seed(4)).to(DEV).to(torch.bfloat16)
+    y = torch.randint(J - 3000, J, (n,), generator=torch.Generator().manual_seed(5), dtype=torch.int32).to(DEV)
+    o = dict(loss=torch.empty(n, device=DEV), lse=torch.empty(n, device=DEV), dA=torch.empty_like(a), dW=torch.empty_like(W))
+    head = sfb.SoftmaxHead(J, D, n)
+    head.loss_and_gradients(W, a, y, **o)
+    head.sync()
+    z = torch.cat([a.double() @ W[i:i + 10000].double().T for i in range(0, J, 10000)], 1)
+    lse = torch.logsumexp(z, 1)
+    u = torch.exp(z - lse[:, None])
+    u[torch.arange(n), y.long()] -= 1.0
+    dA = sum(u[:, i:i + 10000] @ W[i:i + 10000].double() for i in range(0, J, 10000))
+    # scores of some +-2.5 from 16000 products: 1e-5 is twenty deviations of their rounding
+    assert (o["lse"].double() - lse).abs().max() < 1e-5 and (o["loss"].double() - (lse - z[torch.arange(n), y.long()])).abs().max() < 2e-5
+    # results' and U's rounding to bf16: 2^-8 each at most of the largest terms, by norm
+    assert float((o["dA"].double() - dA).norm() / dA.norm()) < 2.0 ** -7
+    for rows in (torch.arange(J - 3000, J, device=DEV), torch.arange(0, 500, device=DEV), torch.arange(134217, 134317, device=DEV)):
+        dW = u[:, rows].T @ a.double()
+        assert float((o["dW"][rows].double() - dW).norm() / dW.norm()) < 2.0 ** -7

@@ -43,6 +43,8 @@ def test_calls_refuse(make, name):
     assert call(w_dtype=5) == -3
     assert call(n=-1) == -2 and call(n=33) == -2
     assert call(ldw=63) == -2 and call(lda=63) == -2
+    for off in ("y", "loss", "lse", "total", "weight"):
+        assert call(**{off: P + 2}) == -1
     assert call(W=P + 1) == -1 and call(a=P + 1) == -1 and call(ws=P + 16) == -1
     assert call(ws=None) == -5 and call(ws_bytes=0) == -5
     grads = C.c_size_t()
@@ -65,6 +67,7 @@ def test_workspace_bytes(make):
     assert lib.sfb_xent_workspace_bytes(ctx(), 7, 1, C.byref(least), C.byref(best)) == -3
     assert lib.sfb_xent_workspace_bytes(ctx(model=sfb.SFB_DML, dtype=sfb.SFB_F32), 1, 1, C.byref(least), C.byref(best)) == -6
     assert lib.sfb_xent_workspace_bytes(ctx(D=(1 << 22) + 1), 1, 1, C.byref(least), C.byref(best)) == -6
+    assert lib.sfb_xent_workspace_bytes(ctx(rows=(1 << 22) + 1), 1, 1, C.byref(least), C.byref(best)) == -6
     # far below the scores and factors themselves: 131072 words, 4096 features, 8192 rows are 4.3 GB of fp32 scores
     big = ctx(J=131072, D=4096, rows=8192)
     for grads in (0, 1):
