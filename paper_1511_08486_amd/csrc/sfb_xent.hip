@@ -627,27 +627,28 @@ __device__ __forceinline__ float xe_top4(f32x4 x, float top) {
 }
 __device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float_as_uint(top) >> 23) - 127 - 14; }   // (2^-126 for all below)
 
-// A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 1024): the first 16 a thread stay
-// in registers between what looks them over and what takes them.
-template <class T, int LANES>
+// A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 1024): the first 4 HELD a thread stay
+// in registers between what looks them over and what takes them (long rows of a large W, all on their way at once, are out of the
+// caches by then: 10000 x 21504 in fp32 452 us with 16 elements a thread).
+template <class T, int LANES, int HELD = 4>
 struct XentRow {
-    f32x4 held[4];
+    f32x4 held[HELD];
     const T* row;
     int D, lane;
     __device__ __forceinline__ XentRow(const T* r, int d) : row(r), D(d), lane(threadIdx.x & (LANES - 1)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) held[i] = load4(row, lane * 4 + 4 * LANES * i, D);
+        for (int i = 0; i < HELD; ++i) held[i] = load4(row, lane * 4 + 4 * LANES * i, D);
     }
     // f(d, four elements from d on), d < whole; zeros from D on
     template <class F>
     __device__ __forceinline__ void each(int64_t whole, F f) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             const int d = lane * 4 + 4 * LANES * i;
             if (d < whole) f(d, held[i]);
         }
 #pragma unroll 4
-        for (int d = lane * 4 + 16 * LANES; d < whole; d += 4 * LANES) f(d, load4(row, d, D));
+        for (int d = lane * 4 + 4 * HELD * LANES; d < whole; d += 4 * LANES) f(d, load4(row, d, D));
     }
     // exponent that brings the largest finite magnitude into [2^14, 2^15) (2^-126 for all below)
     __device__ __forceinline__ int exponent() const {
@@ -731,7 +732,7 @@ struct XentWords {
     int* exps;
 };
 // Row k of W's piece in one bf16 term or (F16) fp16 terms and its exponent; zeros to whole stages and for rows from n on.
-template <class T, bool F16, int LANES>
+template <class T, bool F16, int LANES, int HELD>
 __device__ __forceinline__ void xe_pack_word(const XentWords& p, int k) {
     bf16_t* const out = p.to + (int64_t)k * p.ldd;
     const int lane = threadIdx.x & (LANES - 1);
@@ -740,7 +741,7 @@ __device__ __forceinline__ void xe_pack_word(const XentWords& p, int k) {
         if (F16 && lane == 0) p.exps[k] = -200;                          // below any other: has no say in the largest
         return;
     }
-    const XentRow<T, LANES> row((const T*)p.w + (int64_t)k * p.ld, p.D);
+    const XentRow<T, LANES, HELD> row((const T*)p.w + (int64_t)k * p.ld, p.D);
     if constexpr (F16) {
         const int e0 = row.exponent();
         if (lane == 0) p.exps[k] = e0;
@@ -750,22 +751,37 @@ __device__ __forceinline__ void xe_pack_word(const XentWords& p, int k) {
     }
 }
 // Workgroup b's rows: four short ones (a wavefront each) or one.  The rows are padded to whole multiples of 64.
-constexpr int kXeShortRow = 1024;
-template <class T, bool F16>
+constexpr int kXeShortRow = 1024, kXeLongRow = 8192;
+template <class T, bool F16, bool LONG>
 __device__ __forceinline__ void xe_pack_words(const XentWords& p, int b) {
-    if (p.D <= kXeShortRow) xe_pack_word<T, F16, 64>(p, 4 * b + (threadIdx.x >> 6));
-    else xe_pack_word<T, F16, 256>(p, b);
+    if constexpr (LONG) xe_pack_word<T, F16, 256, 24>(p, b);
+    else if (p.D <= kXeShortRow) xe_pack_word<T, F16, 64, 4>(p, 4 * b + (threadIdx.x >> 6));
+    else xe_pack_word<T, F16, 256, 8>(p, b);
 }
 
 template <class T>
 __global__ __launch_bounds__(256) void xent_pack_rows_kernel(const XentPack p) { xe_pack_row<T>(p, blockIdx.x); }
-template <class T, bool F16>
-__global__ __launch_bounds__(256) void xent_pack_words_kernel(const XentWords w) { xe_pack_words<T, F16>(w, blockIdx.x); }
+template <class T, bool F16, bool LONG>
+__global__ __launch_bounds__(256) void xent_pack_words_kernel(const XentWords w) { xe_pack_words<T, F16, LONG>(w, blockIdx.x); }
 // The rows and the first piece's words in one launch
-template <class TA, class TW, bool F16>
+template <class TA, class TW, bool F16, bool LONG>
 __global__ __launch_bounds__(256) void xent_pack_both_kernel(const XentPack p, const XentWords w) {
     if ((int)blockIdx.x < p.n_padded) xe_pack_row<TA>(p, blockIdx.x);
-    else xe_pack_words<TW, F16>(w, (int)blockIdx.x - p.n_padded);
+    else xe_pack_words<TW, F16, LONG>(w, (int)blockIdx.x - p.n_padded);
+}
+template <bool LONG>
+static void launch_pack_words(const XentWords& w, bool w_bf16, bool f16, uint32_t groups, hipStream_t s) {
+    if (!f16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, false, LONG>), dim3(groups), dim3(256), 0, s, w);
+    else if (w_bf16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true, LONG>), dim3(groups), dim3(256), 0, s, w);
+    else hipLaunchKernelGGL((xent_pack_words_kernel<float, true, LONG>), dim3(groups), dim3(256), 0, s, w);
+}
+template <bool LONG>
+static void launch_pack_both(const XentPack& p, const XentWords& w, bool a_bf16, bool w_bf16, uint32_t groups, hipStream_t s) {
+    const dim3 grid((uint32_t)p.n_padded + groups), block(256);
+    if (a_bf16 && w_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, bf16_t, false, LONG>), grid, block, 0, s, p, w);
+    else if (w_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<float, bf16_t, true, LONG>), grid, block, 0, s, p, w);
+    else if (a_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, float, true, LONG>), grid, block, 0, s, p, w);
+    else hipLaunchKernelGGL((xent_pack_both_kernel<float, float, true, LONG>), grid, block, 0, s, p, w);
 }
 
 // The largest of a piece's exponents
@@ -1303,17 +1319,13 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         there = first;
         const XentWords x{(const char*)c.W + (size_t)first * c.ldw * (c.w_bf16 ? 2 : 4), c.ldw, (int)c.D, (int)n, Wp, l.ld_k, w_plane, l.f16 ? l.w16_terms : 1,
                           l.f16 ? exp_w + first : nullptr};
+        const bool long_rows = c.D > kXeLongRow;
         if (rows_too) {
-            const dim3 grid((uint32_t)(l.n_padded + groups)), block(256);
-            if (!l.f16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, bf16_t, false>), grid, block, 0, s, pack, x);
-            else if (c.w_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<float, bf16_t, true>), grid, block, 0, s, pack, x);
-            else if (c.a_bf16) hipLaunchKernelGGL((xent_pack_both_kernel<bf16_t, float, true>), grid, block, 0, s, pack, x);
-            else hipLaunchKernelGGL((xent_pack_both_kernel<float, float, true>), grid, block, 0, s, pack, x);
+            if (long_rows) launch_pack_both<true>(pack, x, c.a_bf16, c.w_bf16, (uint32_t)groups, s);
+            else launch_pack_both<false>(pack, x, c.a_bf16, c.w_bf16, (uint32_t)groups, s);
         } else {
-            const dim3 grid((uint32_t)groups), block(256);
-            if (!l.f16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, false>), grid, block, 0, s, x);
-            else if (c.w_bf16) hipLaunchKernelGGL((xent_pack_words_kernel<bf16_t, true>), grid, block, 0, s, x);
-            else hipLaunchKernelGGL((xent_pack_words_kernel<float, true>), grid, block, 0, s, x);
+            if (long_rows) launch_pack_words<true>(x, c.w_bf16, l.f16, (uint32_t)groups, s);
+            else launch_pack_words<false>(x, c.w_bf16, l.f16, (uint32_t)groups, s);
         }
         if (l.f16 && grads && !l.kept) hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(1024), 0, s, (const int*)(exp_w + first), (int)n, top);
         return hipGetLastError();

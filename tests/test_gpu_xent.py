@@ -416,3 +416,9 @@ def test_words_beyond_32_bit_offsets():
     for rows in (torch.arange(J - 3000, J, device=DEV), torch.arange(0, 500, device=DEV), torch.arange(134217, 134317, device=DEV)):
         dW = u[:, rows].T @ a.double()
         assert float((o["dW"][rows].double() - dW).norm() / dW.norm()) < 2.0 ** -7
+
+
+@pytest.mark.parametrize("dtype,w_dtype", PAIRS)
+@pytest.mark.parametrize("D", [1023, 1028, 4100, 8191, 8200, 25000])
+def test_rows_of_every_length(D, dtype, w_dtype):
+    _run(20, 70, D, dtype, w_dtype, 42, padded=0.2)
