@@ -153,6 +153,54 @@ __device__ __forceinline__ f32x16 xe_mfma(sp_u32x4 a, sp_u32x4 b, f32x16 c) {
     else return split_mfma(a, b, c);
 }
 
+// A tile's maxima and sums of exponentials by rows, and the scores of labels among its words.  Entry e of acc[i][j]: word
+// m0 + 32 (wm MT + i) + 8 (e / 4) + 4 (lane / 32) + e % 4 of row n0 + 32 (wn NT + j) + lane % 32.
+template <int WGM, int MT, int NT, int BN>
+__device__ __forceinline__ void xe_stats_end(const XentProduct& a, f32x16 (&acc)[MT][NT], int m0, int n0, int wm, int wn, int lane, int count) {
+    constexpr int BM = WGM * MT * 32;
+    extern __shared__ __attribute__((aligned(16))) unsigned char xe_lds[];
+    const int tid = threadIdx.x, l32 = lane & 31, half = lane >> 5;
+    const int mw = m0 + wm * MT * 32 + 4 * half, nw = n0 + wn * NT * 32 + l32;
+            float2* const red = reinterpret_cast<float2*>(xe_lds);
+            const bool inside = m0 + BM <= a.M;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int n = nw + 32 * j;
+                const int hit = n < count ? a.label[n] - a.first_word - mw : -1;         // this lane's offset of the label's word
+                float top = -__builtin_inff(), sum = 0.f, z_hit = 0.f;
+                bool got = false;
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int m = 32 * i + 8 * (e / 4) + e % 4;
+                        if (!inside && mw + m >= a.M) acc[i][j][e] = -__builtin_inff();
+                        top = fmaxf(top, acc[i][j][e]);
+                        if (hit == m) { z_hit = acc[i][j][e]; got = true; }
+                    }
+                const float base = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum += xe_exp(acc[i][j][e] - base);
+                if (got) a.z_label[n] = z_hit;
+                const float top2 = __shfl_xor(top, 32, kWave), sum2 = __shfl_xor(sum, 32, kWave);
+                const float t = fmaxf(top, top2), b = t == -__builtin_inff() ? 0.f : t;
+                sum = sum * xe_exp(top - b) + sum2 * xe_exp(top2 - b);
+                if (half == 0) red[wm * BN + wn * NT * 32 + 32 * j + l32] = make_float2(t, sum);
+            }
+            __syncthreads();
+            for (int n = tid; n < BN; n += blockDim.x) {
+                float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < WGM; ++w) top = fmaxf(top, red[w * BN + n].x);
+                const float base = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < WGM; ++w) sum += red[w * BN + n].y * xe_exp(red[w * BN + n].x - base);
+                if (n0 + n < count) a.partial[(int64_t)(n0 + n) * a.ld_partial + m0 / BM] = make_float2(top, sum);
+            }
+}
+
 // F16: operands in fp16 terms, exponents beside them; the products of a second term come first and are 2^11 times as large
 template <int WGM, int WGN, int MT, int NT, int ST, int OCC, bool XT, bool YT, bool F16, int END, class Out>
 __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const XentProduct a) {
@@ -362,44 +410,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
             }
     }
     if constexpr (END == kXeStats) {
-        float2* const red = reinterpret_cast<float2*>(xe_lds);
-        const bool inside = m0 + BM <= a.M;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int n = nw + 32 * j;
-            const int hit = n < count ? a.label[n] - a.first_word - mw : -1;         // this lane's offset of the label's word
-            float top = -__builtin_inff(), sum = 0.f, z_hit = 0.f;
-            bool got = false;
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int m = 32 * i + 8 * (e / 4) + e % 4;
-                    if (!inside && mw + m >= a.M) acc[i][j][e] = -__builtin_inff();
-                    top = fmaxf(top, acc[i][j][e]);
-                    if (hit == m) { z_hit = acc[i][j][e]; got = true; }
-                }
-            const float base = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sum += xe_exp(acc[i][j][e] - base);
-            if (got) a.z_label[n] = z_hit;
-            const float top2 = __shfl_xor(top, 32, kWave), sum2 = __shfl_xor(sum, 32, kWave);
-            const float t = fmaxf(top, top2), b = t == -__builtin_inff() ? 0.f : t;
-            sum = sum * xe_exp(top - b) + sum2 * xe_exp(top2 - b);
-            if (half == 0) red[wm * BN + wn * NT * 32 + 32 * j + l32] = make_float2(t, sum);
-        }
-        __syncthreads();
-        for (int n = tid; n < BN; n += WAVES * 64) {
-            float top = -__builtin_inff(), sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < WGM; ++w) top = fmaxf(top, red[w * BN + n].x);
-            const float base = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-            for (int w = 0; w < WGM; ++w) sum += red[w * BN + n].y * xe_exp(red[w * BN + n].x - base);
-            if (n0 + n < count) a.partial[(int64_t)(n0 + n) * a.ld_partial + m0 / BM] = make_float2(top, sum);
-        }
+        xe_stats_end<WGM, MT, NT, BN>(a, acc, m0, n0, wm, wn, lane, count);
     } else if constexpr (END == kXeU) {
         constexpr int PER = BM / 8;                                      // 16-byte pieces of an LDS row
         static_assert(BN * BM * 2 <= ST * STAGE, "the tile of U in one go");
@@ -530,6 +541,106 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
     }
 }
 
+// Scores of up to 64 rows with W in fp32 as it is: W goes to LDS raw and is split into three bf16 terms on its way to the matrix cores
+// (exact; six products with fp32 features, three with bf16 ones), so that it crosses memory once.  By the general way its terms are
+// written and read again.  128 words a workgroup, a stage of 64 k with all of the features' terms, three
+// stages (two of 33 to 64 rows in three terms); the leading products and the others in sums of their own, the former in blocks of 256 k.
+// LDS rows of W: 256 bytes, 16-byte piece p of row r at p ^ (r & 15).
+constexpr int kXeRawWords = 128;
+template <int NT, int TERMS> constexpr int kXeRawStages = NT == 2 && TERMS == 3 ? 2 : 3;
+
+template <int NT, int TERMS>
+__global__ __launch_bounds__(256, 1) void xent_raw_scores_kernel(const XentProduct a) {
+    constexpr int X_BYTES = kXeRawWords * 256, Y_BYTES = NT * 32 * 128, STAGE = X_BYTES + TERMS * Y_BYTES, LOADS = 8 + TERMS * NT, ST = kXeRawStages<NT, TERMS>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char xe_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5, m0 = blockIdx.x * kXeRawWords, count = *a.count;
+    if (count == 0) return;
+    const float* const W = reinterpret_cast<const float*>(a.x) + (int64_t)m0 * a.ldx;
+    uint32_t x_off[8], y_off[NT];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {                                        // 16 rows of W an access of the four wavefronts
+        const int in16 = wave * 4 + (lane >> 4), r = min(m0 + i * 16 + in16, a.x_rows - 1) - m0;
+        x_off[i] = (uint32_t)r * (uint32_t)a.ldx * 4u + (uint32_t)(((lane & 15) ^ in16) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+        y_off[i] = (uint32_t)((i * 4 + wave) * 8 + (lane >> 3)) * (uint32_t)a.ldy * 2u + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7) ^ (wave & 1)) * 16);
+    const uint32_t lds0 = xe_lds_address(xe_lds);
+    const int stages = a.k_tiles;
+    auto request = [&](int s) {
+        const bool last = s == stages - 1;
+        const uint32_t to = lds0 + (s % ST) * STAGE;
+        const float* const x = W + (last ? a.last_x : s * kXeK);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xe_dma(x, x_off[i], to + (i * 4 + wave) * 1024);
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            const bf16_t* const y = a.y + t * a.y_plane + (last ? a.last_y : s * kXeK);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) xe_dma(y, y_off[i], to + X_BYTES + t * Y_BYTES + (i * 4 + wave) * 1024);
+        }
+    };
+    f32x16 acc[1][NT], sum[NT], small[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[0][j][e] = sum[j][e] = small[j][e] = 0.f;
+    for (int s = 0; s < min(ST - 1, stages); ++s) request(s);
+    for (int s = 0; s < stages; ++s) {
+        if (s + 1 < stages) xe_stage_barrier<(ST - 2) * LOADS>();        // this stage is there, the next of three may be on its way
+        else xe_wait_barrier();
+        if (s + ST - 1 < stages) request(s + ST - 1);                    // into the buffer that everybody is through with
+        const unsigned char* const now = xe_lds + (s % ST) * STAGE;
+        const unsigned char* const w_row = now + (wave * 32 + l32) * 256;
+        split_for<0, 4>([&](auto sc) {
+            constexpr int ks = decltype(sc)::value;
+            f32x4 v[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) v[q] = *reinterpret_cast<const f32x4*>(w_row + (((4 * ks + 2 * half + q) ^ (l32 & 15)) << 4));
+            sp_u32x4 w[3];
+#pragma unroll
+            for (int t = 0; t < 3; ++t)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    float x[4] = {v[q][0], v[q][1], v[q][2], v[q][3]};
+                    const uint2 b = xe_bf4(x);
+                    w[t][2 * q] = b.x;
+                    w[t][2 * q + 1] = b.y;
+                    v[q] = f32x4{x[0], x[1], x[2], x[3]};
+                }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                sp_u32x4 y[TERMS];
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+                    y[t] = *reinterpret_cast<const sp_u32x4*>(now + X_BYTES + t * Y_BYTES + (j * 32 + l32) * 128 +
+                                                              (((2 * ks + half) ^ (l32 & 7) ^ ((l32 >> 3) & 1)) << 4));
+                small[j] = split_mfma(w[2], y[0], small[j]);
+                if constexpr (TERMS == 3) {
+                    small[j] = split_mfma(w[0], y[2], small[j]);
+                    small[j] = split_mfma(w[1], y[1], small[j]);
+                    small[j] = split_mfma(w[0], y[1], small[j]);
+                }
+                small[j] = split_mfma(w[1], y[0], small[j]);
+                acc[0][j] = split_mfma(w[0], y[0], acc[0][j]);
+            }
+        });
+        if ((s & 3) == 3) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                sum[j] += acc[0][j];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[0][j][e] = 0.f;
+            }
+        }
+    }
+    xe_wait_barrier();
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[0][j] += sum[j] + small[j];
+    xe_stats_end<4, 1, NT, NT * 32>(a, acc, m0, 0, wave, 0, lane, count);
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // What stands around the products
 
@@ -629,7 +740,7 @@ __device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float
 
 // A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 1024): the first 4 HELD a thread stay
 // in registers between what looks them over and what takes them (long rows of a large W, all on their way at once, are out of the
-// caches by then: 10000 x 21504 in fp32 452 us with 16 elements a thread).
+// caches by then: 10000 x 21504 in fp32 452 us with 16 elements a thread, 371 with 96).
 template <class T, int LANES, int HELD = 4>
 struct XentRow {
     f32x4 held[HELD];
@@ -715,10 +826,10 @@ __device__ __forceinline__ void xe_pack_row(const XentPack& p, int k) {
         xe_put(to + d, p.plane, p.terms, v);
     });
     if (p.window && tid < 16) {
-        const int d = p.D - 64 + tid * 4;                                // D is a multiple of 8 here
+        const int d = p.D - 64 + tid * 4;                                // D is a multiple of 4 here
         f32x4 v = load4(src, d, p.D);
         if (d < p.window - 64) v = f32x4{0.f, 0.f, 0.f, 0.f};
-        xe_put(to + p.window + tid * 4, 0, 1, v);
+        xe_put(to + p.window + tid * 4, p.plane, p.terms, v);
     }
 }
 
@@ -1011,21 +1122,40 @@ static hipError_t launch_tiles(XentProduct a, hipStream_t s) {
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     auto* const kernel = &xent_product_kernel<WGM, WGN, MT, NT, ST, OCC, XT, YT, F16, END, Out>;
     if constexpr (lds > 64 * 1024) {
-        static std::atomic<uint64_t> raised{0};                          // GPUs that know
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
+        static std::atomic<uint64_t> raised{0};
+        const hipError_t e = raise_lds(kernel, lds, raised);
         if (e != hipSuccess) return e;
-        if (dev > 63 || !(raised.load() >> dev & 1)) {
-            e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            if (e != hipSuccess) return e;
-            if (dev <= 63) raised |= 1ull << dev;
-        }
     }
     a.m_tiles = (a.M + BM - 1) / BM;
     a.n_tiles = (a.N + BN - 1) / BN;
     a.total = a.m_tiles * a.n_tiles * a.splits;
     a.per_split = (a.k_tiles + a.splits - 1) / a.splits;
     SFB_LAUNCH((xent_product_kernel<WGM, WGN, MT, NT, ST, OCC, XT, YT, F16, END, Out>), dim3(a.total), dim3(WGM * WGN * 64), lds, s, a);
+    return hipGetLastError();
+}
+
+// Largest dynamic LDS of a kernel beyond 64 KB, told to the runtime once for every GPU.
+template <class K>
+static hipError_t raise_lds(K* kernel, size_t lds, std::atomic<uint64_t>& raised) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev > 63 || !(raised.load() >> dev & 1)) {
+        e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        if (dev <= 63) raised |= 1ull << dev;
+    }
+    return hipSuccess;
+}
+
+template <int NT, int TERMS>
+static hipError_t launch_raw_scores(const XentProduct& a, hipStream_t s) {
+    constexpr size_t lds = (size_t)kXeRawStages<NT, TERMS> * (kXeRawWords * 256 + TERMS * NT * 32 * 128);
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    static std::atomic<uint64_t> raised{0};
+    const hipError_t e = raise_lds(&xent_raw_scores_kernel<NT, TERMS>, lds, raised);
+    if (e != hipSuccess) return e;
+    SFB_LAUNCH((xent_raw_scores_kernel<NT, TERMS>), dim3((uint32_t)((a.M + kXeRawWords - 1) / kXeRawWords)), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 
@@ -1121,7 +1251,7 @@ constexpr size_t kXePieceBytes = (size_t)512 << 20, kXeScoreBytes = (size_t)256 
 // What a call does and where it keeps it.
 struct Layout {
     int64_t n_padded, piece, ld_k, ld_a, ld_acc, ld_z, ld_partial; // piece: words; ld_k: features to whole stages
-    bool f16, direct, kept;                            // fp16 terms (either operand fp32); W read as it is; scores of all words kept
+    bool f16, direct, kept, raw;                       // fp16 terms (either operand fp32); W read as it is; scores of all words kept; fp32 W as it is
     int k_tiles, window;
     int a_terms, a16_terms, w16_terms, u_terms, u16_terms;
     int score_most, dA_most, dW_most;                  // pairs of terms
@@ -1130,15 +1260,19 @@ struct Layout {
 };
 }  // namespace
 
-static bool reads_w_directly(const XentCall& c) {
-    return c.w_bf16 && c.a_bf16 && c.D % 8 == 0 && c.D >= 64 && c.ldw % 8 == 0 && ((uintptr_t)c.W % 16) == 0 && c.ldw < (1 << 23);
+// Rows of W that a product reads as they are: in bf16 with bf16 features; in fp32 for the loss of few rows.  Pieces of 16 bytes, 32-bit offsets.
+static bool reads_w_directly(const XentCall& c, bool grads) {
+    if (c.D < 64 || ((uintptr_t)c.W % 16) != 0 || c.ldw >= (1 << 22)) return false;
+    if (c.w_bf16) return c.a_bf16 && c.D % 8 == 0 && c.ldw % 8 == 0;
+    return !grads && c.n <= 64 && c.D % 4 == 0 && c.ldw % 4 == 0;
 }
 
 // piece: words of a piece, a multiple of 256
 static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, int64_t piece) {
     Layout l{};
     const int64_t n = c.n > 0 ? c.n : 1, words = piece < c.J ? piece : c.J;
-    l.f16 = !(c.a_bf16 && c.w_bf16);
+    l.raw = direct && !c.w_bf16;
+    l.f16 = !l.raw && !(c.a_bf16 && c.w_bf16);
     l.direct = direct;
     l.kept = kept;
     l.piece = piece;
@@ -1158,7 +1292,7 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
         l.u_terms = grads ? l.dW_most + 1 : 0;
         l.a_terms = grads ? (c.a_bf16 ? 1 : l.dW_most + 1) : 0;
     } else {
-        l.a_terms = 1;
+        l.a_terms = l.raw && !c.a_bf16 ? 3 : 1;
         l.u_terms = grads ? 1 : 0;
     }
     const int score_pairs = l.f16 ? pair_count(l.w16_terms, l.a16_terms, 1) : 1;
@@ -1257,6 +1391,11 @@ size_t xent_workspace(const XentCall& c, bool grads, bool least) {
         if (b > m) m = b;
     }
     if (least) return m;
+    if (!grads && !c.w_bf16 && c.n <= 64 && c.D % 4 == 0 && c.D >= 64) { // fp32 W read as it is; pieces for rows that lie otherwise
+        const int64_t whole = up(c.J, 256);
+        const size_t b = layout_of(c, true, false, false, whole).bytes, o = layout_of(c, false, false, false, whole < 8192 ? whole : 8192).bytes;
+        return b > m ? (b > o ? b : o) : (m > o ? m : o);
+    }
     for (int f = 0; f < 2; ++f) {
         const size_t b = plan_call(c, direct, f != 0, grads, ~(size_t)0).bytes;
         if (b > m) m = b;
@@ -1265,7 +1404,7 @@ size_t xent_workspace(const XentCall& c, bool grads, bool least) {
 }
 
 hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t s) {
-    const bool direct = reads_w_directly(c);
+    const bool direct = reads_w_directly(c, grads);
     const Layout l = plan_call(c, direct, forward, grads, c.ws_bytes);
     if (l.bytes > c.ws_bytes) return hipErrorInvalidValue;
     char* const ws = (char*)c.ws;
@@ -1308,8 +1447,9 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     auto words = [&](int64_t first, int64_t n, Words* w) -> hipError_t {
         const bool rows_too = there < 0;
         if (direct) {
-            *w = Words{(const bf16_t*)c.W + first * c.ldw, c.ldw, 0, (int)n};
-            if (rows_too) hipLaunchKernelGGL(xent_pack_rows_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, pack);
+            *w = Words{(const bf16_t*)((const char*)c.W + (size_t)first * c.ldw * (c.w_bf16 ? 2 : 4)), c.ldw, 0, (int)n};
+            if (rows_too && c.a_bf16) hipLaunchKernelGGL(xent_pack_rows_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, pack);
+            if (rows_too && !c.a_bf16) hipLaunchKernelGGL(xent_pack_rows_kernel<float>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, pack);
             there = 0;
             return rows_too ? hipGetLastError() : hipSuccess;
         }
@@ -1390,10 +1530,16 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             if (e != hipSuccess) return e;
             scores_of(first, n, w);
             scores.partial = (float2*)(ws + l.partial) + tiles;
-            e = l.f16 ? launch_product<false, false, true, kXeStats, float>(scores, l.scores.tile, s)
-                      : launch_product<false, false, false, kXeStats, float>(scores, l.scores.tile, s);
+            if (l.raw) {
+                e = c.a_bf16 ? (n_some > 32 ? launch_raw_scores<2, 1>(scores, s) : launch_raw_scores<1, 1>(scores, s))
+                             : (n_some > 32 ? launch_raw_scores<2, 3>(scores, s) : launch_raw_scores<1, 3>(scores, s));
+            } else {
+                e = l.f16 ? launch_product<false, false, true, kXeStats, float>(scores, l.scores.tile, s)
+                          : launch_product<false, false, false, kXeStats, float>(scores, l.scores.tile, s);
+            }
             if (e != hipSuccess) return e;
-            tiles += (int)((n + kXeTileM[l.scores.tile] - 1) / kXeTileM[l.scores.tile]);
+            const int tile_m = l.raw ? kXeRawWords : kXeTileM[l.scores.tile];
+            tiles += (int)((n + tile_m - 1) / tile_m);
         }
         // (64 rows are four a wavefront of one workgroup, which then needs no launch behind it for the total)
         const bool alone = n_some <= 64;

@@ -422,3 +422,19 @@ def test_words_beyond_32_bit_offsets():
 @pytest.mark.parametrize("D", [1023, 1028, 4100, 8191, 8200, 25000])
 def test_rows_of_every_length(D, dtype, w_dtype):
     _run(20, 70, D, dtype, w_dtype, 42, padded=0.2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,J,D,pad", [(1, 500, 64, 0), (1, 129, 68, 0), (7, 1000, 132, 4), (32, 300, 320, 0), (33, 257, 256, 8), (64, 5000, 1100, 0), (20, 700, 4096, 0),
+                                       (20, 700, 100, 1), (64, 300, 66, 0), (5, 40, 60, 0)])
+def test_loss_of_few_rows_with_fp32_words(n, J, D, pad, dtype):
+    """W in fp32 read as it is (whole multiples of 4 features at 16-byte rows), and where it cannot be."""
+    import paper_1511_08486_amd as sfb
+    W, a, y = _inputs(n, J, D, dtype, "f32", 50 + n, pad=pad, padded=0.2 if n > 1 else 0.0, spread=3.0)
+    weight = torch.rand(n, generator=torch.Generator().manual_seed(1)).to(DEV)
+    head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype="f32", gradients=False)
+    head._ws.fill_(255)
+    o = dict(loss=torch.full((n,), 7.0, device=DEV), lse=torch.full((n,), 7.0, device=DEV), total=torch.zeros(1, device=DEV))
+    head.loss(W, a, y, **o, weight=weight, mean=True)
+    head.sync()
+    _check(o, _formula(W, a, y, weight, mean=True), dtype, "f32", D, f"{n} {J} {D}")
