@@ -543,11 +543,12 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
 
 // Scores of up to 64 rows with W in fp32 as it is: W goes to LDS raw and is split into three bf16 terms on its way to the matrix cores
 // (exact; six products with fp32 features, three with bf16 ones), so that it crosses memory once.  By the general way its terms are
-// written and read again.  128 words a workgroup, a stage of 64 k with all of the features' terms, three
-// stages (two of 33 to 64 rows in three terms); the leading products and the others in sums of their own, the former in blocks of 256 k.
+// written and read again.  128 words a workgroup, a stage of 64 k with all of the features' terms; two
+// stages, so that two workgroups fit a compute unit (65536 x 4096, one row of bf16: 235 us, 4.6 TB/s; one workgroup with three or four stages
+// 289; its terms packed first 728), three where only one fits anyway (fp32 features: 290; packed 917).  The leading products and the others have sums of their own, the former in blocks of 256 k.
 // LDS rows of W: 256 bytes, 16-byte piece p of row r at p ^ (r & 15).
 constexpr int kXeRawWords = 128;
-template <int NT, int TERMS> constexpr int kXeRawStages = NT == 2 && TERMS == 3 ? 2 : 3;
+template <int NT, int TERMS> constexpr int kXeRawStages = TERMS == 3 && NT == 1 ? 3 : 2;
 
 template <int NT, int TERMS>
 __global__ __launch_bounds__(256, 1) void xent_raw_scores_kernel(const XentProduct a) {
