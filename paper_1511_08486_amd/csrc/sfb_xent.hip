@@ -739,7 +739,7 @@ __device__ __forceinline__ float xe_top4(f32x4 x, float top) {
 }
 __device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float_as_uint(top) >> 23) - 127 - 14; }   // (2^-126 for all below)
 
-// A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 1024): the first 4 HELD a thread stay
+// A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 2048): the first 4 HELD a thread stay
 // in registers between what looks them over and what takes them (long rows of a large W, all on their way at once, are out of the
 // caches by then: 10000 x 21504 in fp32 452 us with 16 elements a thread, 371 with 96).
 template <class T, int LANES, int HELD = 4>
@@ -863,12 +863,13 @@ __device__ __forceinline__ void xe_pack_word(const XentWords& p, int k) {
     }
 }
 // Workgroup b's rows: four short ones (a wavefront each) or one.  The rows are padded to whole multiples of 64.
-constexpr int kXeShortRow = 1024, kXeLongRow = 8192;
+constexpr int kXeShortRow = 2048, kXeLongRow = 4096;
 template <class T, bool F16, bool LONG>
 __device__ __forceinline__ void xe_pack_words(const XentWords& p, int b) {
     if constexpr (LONG) xe_pack_word<T, F16, 256, 24>(p, b);
-    else if (p.D <= kXeShortRow) xe_pack_word<T, F16, 64, 4>(p, 4 * b + (threadIdx.x >> 6));
-    else xe_pack_word<T, F16, 256, 8>(p, b);
+    else if (p.D <= kXeShortRow / 2) xe_pack_word<T, F16, 64, 4>(p, 4 * b + (threadIdx.x >> 6));
+    else if (p.D <= kXeShortRow) xe_pack_word<T, F16, 64, 8>(p, 4 * b + (threadIdx.x >> 6));
+    else xe_pack_word<T, F16, 256, 4>(p, b);
 }
 
 template <class T>
