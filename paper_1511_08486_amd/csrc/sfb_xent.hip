@@ -1372,6 +1372,7 @@ static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads
         int64_t lo = 1, hi = whole < (1 << 14) ? whole : (1 << 14);      // 32-bit offsets inside a tile: 2^22 words at most
         if (u_bytes > 0 && hi > (int64_t)(kXePieceBytes / u_bytes)) hi = (int64_t)(kXePieceBytes / u_bytes);
         if (w_bytes > 0 && hi > (int64_t)(kXeWordBytes / w_bytes)) hi = (int64_t)(kXeWordBytes / w_bytes);
+        if (hi < 1) hi = 1;
         if (layout_of(c, direct, grads, kept != 0, hi * 256).bytes <= bytes) lo = hi;    // (bytes may fall as pieces grow: fewer splits of dA)
         while (lo < hi) {
             const int64_t mid = (lo + hi + 1) / 2;

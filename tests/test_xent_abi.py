@@ -68,6 +68,10 @@ def test_workspace_bytes(make):
     assert lib.sfb_xent_workspace_bytes(ctx(model=sfb.SFB_DML, dtype=sfb.SFB_F32), 1, 1, C.byref(least), C.byref(best)) == -6
     assert lib.sfb_xent_workspace_bytes(ctx(D=(1 << 22) + 1), 1, 1, C.byref(least), C.byref(best)) == -6
     assert lib.sfb_xent_workspace_bytes(ctx(rows=(1 << 22) + 1), 1, 1, C.byref(least), C.byref(best)) == -6
+    # one piece of 256 words beyond the bounds that pieces are cut to
+    for c, w in ((ctx(rows=1 << 22, dtype=sfb.SFB_F32, J=100000), 0), (ctx(D=1 << 22, rows=8, dtype=sfb.SFB_F32, J=100000), 0), (ctx(rows=1 << 22, J=100000), 1)):
+        for grads in (0, 1):
+            assert lib.sfb_xent_workspace_bytes(c, w, grads, C.byref(least), C.byref(best)) == 0 and 0 < least.value <= best.value
     # far below the scores and factors themselves: 131072 words, 4096 features, 8192 rows are 4.3 GB of fp32 scores
     big = ctx(J=131072, D=4096, rows=8192)
     for grads in (0, 1):
