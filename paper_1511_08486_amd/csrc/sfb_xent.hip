@@ -64,6 +64,8 @@ struct XentProduct {
     const float* add;                        // fp32, or nullptr
     int64_t ld_add;
     const int* row_map;                      // row of out for n, or nullptr
+    const float *loss_packed, *weights;      // of the total, if the first workgroup is to form that
+    float* loss_total;
 };
 
 __device__ __forceinline__ uint32_t xe_lds_address(const void* p) {
@@ -205,6 +207,22 @@ __device__ __forceinline__ void xe_stats_end(const XentProduct& a, f32x16 (&acc)
             }
 }
 
+// total = f sum of g loss in a fixed order, in 64 bits, by one workgroup; `part`: 8 bytes of LDS a wavefront
+__device__ __forceinline__ void xe_total(const float* loss, const float* g, int n, const float* factor, float* total, double* part) {
+    double s = 0.0;
+    for (int k = threadIdx.x; k < n; k += blockDim.x) s += (double)loss[k] * (double)g[k];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.0;
+        for (int w = 0; w < (int)blockDim.x / 64; ++w) s += part[w];
+        *total = (float)(s * (double)*factor);
+    }
+    __syncthreads();
+}
+
 // F16: operands in fp16 terms, exponents beside them; the products of a second term come first and are 2^11 times as large
 template <int WGM, int WGN, int MT, int NT, int ST, int OCC, bool XT, bool YT, bool F16, int END, class Out>
 __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const XentProduct a) {
@@ -224,6 +242,9 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
     const int m0 = (8 * band + in_band % wide) * BM, n0 = in_band / wide * BN;
 
     const int count = *a.count;
+    if constexpr (END == kXeStore) {
+        if (a.loss_total && blockIdx.x == 0) xe_total(a.loss_packed, a.weights, count, a.factor, a.loss_total, reinterpret_cast<double*>(xe_lds));
+    }
     if (a.n_is_rows && n0 >= count) return;
     const int k_tiles = a.k_is_rows ? (count + kXeK - 1) / kXeK : a.k_tiles;
     const int k_begin = min(split * a.per_split, k_tiles), k_end = min(k_begin + a.per_split, k_tiles);
@@ -1036,22 +1057,6 @@ __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows 
     }
 }
 
-// total = f sum of g loss in a fixed order, in 64 bits; a workgroup of 1024
-__device__ __forceinline__ void xe_total(const float* loss, const float* g, int n, const float* factor, float* total) {
-    __shared__ double part[16];
-    double s = 0.0;
-    for (int k = threadIdx.x; k < n; k += 1024) s += (double)loss[k] * (double)g[k];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s = 0.0;
-        for (int w = 0; w < 16; ++w) s += part[w];
-        *total = (float)(s * (double)*factor);
-    }
-}
-
 // lse and loss of a row from its tiles' maxima and sums: a wavefront a row, tiles in a fixed order.  One workgroup alone adds up the total
 // as well (total not null).
 __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_partial, const int* __restrict__ rows,
@@ -1086,14 +1091,16 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restric
         }
     }
     if (total) {
+        __shared__ double part[16];
         __syncthreads();
-        xe_total(loss_packed, g, count, factor, total);
+        xe_total(loss_packed, g, count, factor, total, part);
     }
 }
 
 __global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restrict__ loss, const float* __restrict__ g, const int* __restrict__ count,
                                                           const float* __restrict__ factor, float* __restrict__ total) {
-    xe_total(loss, g, *count, factor, total);
+    __shared__ double part[16];
+    xe_total(loss, g, *count, factor, total, part);
 }
 
 // dA's rows from the accumulators' planes
@@ -1349,18 +1356,21 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
 
 // Whether a call keeps its scores: they fit, and forming them again (or leaving most compute units idle) would take longer than their
 // way to memory and back.  A score costs 2 D flops a pair of terms again, at about 1.1 PFLOP/s, or some 12 bytes at 4 TB/s.
+// Measured, kept and not, bf16: both directions, 32 rows, 65536 x 4096: 450 us and 532; 64 rows, 1000 x 2048: 35 and 71; one, 32000 x 1504:
+// 88 and 95.  The loss alone splits k over idle units: 64 rows, 8000 x 4096: 32 and 50; one, 1000 x 4096: 16 and 31; where it gains least
+// (one row, 8000 x 1504) the pass over the scores costs more than that: 22 and 19.
 static bool keeps_scores(const XentCall& c, bool forward, bool grads) {
     const int64_t n = c.n > 0 ? c.n : 1, whole = up(c.J, 256);
     if ((size_t)up(n, 256) * whole * 4 > kXeScoreBytes) return false;
     const int pairs = c.a_bf16 && c.w_bf16 ? 1 : c.a_bf16 || c.w_bf16 ? 2 : 3;
     const int64_t tiles = ((c.J + 127) / 128) * ((n + 127) / 128);
-    return n > 64 && c.D * pairs >= 1500 && ((forward && grads) || tiles < 200);
+    return c.D * pairs >= 1500 && ((forward && grads) || tiles < (n > 64 ? 200 : 64));
 }
 
 // The layout that a call on c's sizes takes within `bytes`; .bytes > bytes: there is none
 static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads, size_t bytes) {
     const int64_t whole = up(c.J, 256) / 256;
-    for (int kept = keeps_scores(c, forward, grads); kept >= 0; --kept) {
+    for (int kept = !(direct && !c.w_bf16) && keeps_scores(c, forward, grads); kept >= 0; --kept) {
         if (!grads && direct) {
             const Layout l = layout_of(c, true, false, kept != 0, whole * 256);
             if (l.bytes <= bytes || !kept) return l;
@@ -1555,7 +1565,9 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
                            (const float*)factor, alone ? c.total : nullptr);
         total_done = alone;
     }
-    if (forward && c.total && !total_done)
+    // with gradients the first workgroup of their first product does it
+    float* total_left = forward && !total_done && grads ? c.total : nullptr;
+    if (forward && c.total && !total_done && !grads)
         hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, (const float*)factor, c.total);
     e = hipGetLastError();
     if (e != hipSuccess || !grads) return e;
@@ -1593,6 +1605,8 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
                 p.out = ws + l.acc; p.ldo = l.ld_acc; p.out_plane = acc_plane;
             }
             p.add = i < pieces - 1 ? (const float*)(ws + l.acc) : nullptr; p.ld_add = l.ld_acc;
+            p.loss_packed = loss; p.weights = g; p.loss_total = total_left;
+            total_left = nullptr;
             if (p.row_map && c.a_bf16)
                 e = l.f16 ? launch_product<true, false, true, kXeStore, bf16_t>(p, l.dA.tile, s) : launch_product<true, false, false, kXeStore, bf16_t>(p, l.dA.tile, s);
             else
@@ -1610,6 +1624,8 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             p.count = count; p.k_is_rows = true;
             p.factor = factor;
             p.ldo = c.lddw;
+            p.loss_packed = loss; p.weights = g; p.loss_total = total_left;
+            total_left = nullptr;
             if (c.w_bf16) {
                 p.out = (bf16_t*)c.dW + first * c.lddw;
                 e = launch_product<true, true, false, kXeStore, bf16_t>(p, l.dW.tile, s);

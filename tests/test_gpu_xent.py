@@ -153,6 +153,13 @@ def test_long_features(two, dtype, w_dtype):
 
 
 @pytest.mark.parametrize("dtype,w_dtype", PAIRS)
+@pytest.mark.parametrize("n,J,D", [(1, 1000, 2048), (40, 5000, 1600), (64, 300, 4096), (33, 70000, 1536)])
+def test_few_rows_of_long_features(n, J, D, dtype, w_dtype):
+    _run(n, J, D, dtype, w_dtype, seed=32, padded=0.1 if n > 1 else 0.0)
+    _run(n, J, D, dtype, w_dtype, seed=32, padded=0.1 if n > 1 else 0.0, two=True)
+
+
+@pytest.mark.parametrize("dtype,w_dtype", PAIRS)
 def test_rows_and_words_of_very_different_size(dtype, w_dtype):
     """Rows of a and of W 2^-20 to 2^20 of their neighbours', scores of ordinary size all the same."""
     import paper_1511_08486_amd as sfb
