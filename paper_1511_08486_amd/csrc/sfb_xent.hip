@@ -44,7 +44,7 @@ struct XentProduct {
     uint32_t pair_x, pair_y;                 // four bits a pair: the terms of X and Y, in order
     const int *exp_m, *exp_n, *exp_top;      // fp16 terms: results are times 2^(exp_m[m] + exp_n[n] + *exp_top); null: 0
     int m_tiles, n_tiles, total, splits, per_split;
-    const int* count;                        // rows that take part
+    const int* count;                        // rows that take part; null: all N
     bool n_is_rows, k_is_rows;               // what `count` bounds
     // kXeStats, kXeU
     const int* label;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
     const int band = id / (8 * a.n_tiles), in_band = id - band * (8 * a.n_tiles), wide = min(8, a.m_tiles - 8 * band);
     const int m0 = (8 * band + in_band % wide) * BM, n0 = in_band / wide * BN;
 
-    const int count = *a.count;
+    const int count = a.count ? *a.count : a.N;
     if constexpr (END == kXeStore) {
         if (a.loss_total && blockIdx.x == 0) xe_total(a.loss_packed, a.weights, count, a.factor, a.loss_total, reinterpret_cast<double*>(xe_lds));
     }
@@ -1057,6 +1057,55 @@ __global__ __launch_bounds__(kXeRowThreads) void xent_row_kernel(const XentRows 
     }
 }
 
+// Maximum of a row's scores and sum of their exponentials under it from its tiles', in a fixed order, by a wavefront
+__device__ __forceinline__ float2 xe_join(const float2* __restrict__ partial, int tiles, int lane) {
+    float top = -__builtin_inff(), sum = 0.f;
+    for (int t = lane; t < tiles; t += 512) {                            // eight on their way at a time
+        float2 p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = t + 64 * i < tiles ? partial[t + 64 * i] : make_float2(-__builtin_inff(), 0.f);
+        float m = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i].x);
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        sum *= xe_exp(top - base);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += p[i].y * xe_exp(p[i].x - base);
+        top = m;
+    }
+    const float most = wave_max(top), base = most == -__builtin_inff() ? 0.f : most;
+    return make_float2(most, wave_sum(sum * xe_exp(top - base)));
+}
+
+// The same of up to 64 rows that were read where they lie, by one workgroup: row k of the partial sums is row k of the call, and what those
+// that take no part left there (it may be NaN) is dropped here.
+__global__ __launch_bounds__(1024) void xent_in_place_loss_kernel(const XentPack p, const float2* __restrict__ partial, int tiles, int ld_partial,
+                                                                  const float* __restrict__ z_label, float* __restrict__ loss, float* __restrict__ lse,
+                                                                  float* __restrict__ total) {
+    __shared__ float found[64];
+    const int lane = threadIdx.x & 63;
+    for (int k = threadIdx.x >> 6; k < p.n; k += 16) {
+        const int label = p.y[k];
+        const bool real = label >= 0 && label < p.J;
+        const float2 s = xe_join(partial + (int64_t)k * ld_partial, tiles, lane);
+        if (lane == 0) {
+            const float l = logf(s.y), f = real ? l + (s.x - z_label[k]) : 0.f;
+            if (lse) lse[k] = real ? s.x + l : 0.f;
+            if (loss) loss[k] = f;
+            found[k] = f;
+        }
+    }
+    __syncthreads();
+    if (!total || threadIdx.x >= 64) return;
+    const int label = lane < p.n ? p.y[lane] : -1;
+    const bool real = label >= 0 && label < p.J;
+    const int count = __popcll(__ballot(real));
+    double s = real ? (double)found[lane] * (double)(p.weight ? p.weight[lane] : 1.f) : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
+    if (lane == 0) *total = (float)(s * (double)(p.mean && count > 0 ? p.scale / (float)count : p.scale));
+}
+
 // lse and loss of a row from its tiles' maxima and sums: a wavefront a row, tiles in a fixed order.  One workgroup alone adds up the total
 // as well (total not null).
 __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restrict__ partial, int tiles, int ld_partial, const int* __restrict__ rows,
@@ -1065,24 +1114,9 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(const float2* __restric
                                                          const float* __restrict__ factor, float* __restrict__ total) {
     const int lane = threadIdx.x & 63, count = *counted;
     for (int k = blockIdx.x * 16 + (threadIdx.x >> 6); k < count; k += gridDim.x * 16) {
-        float top = -__builtin_inff(), sum = 0.f;
-        for (int t = lane; t < tiles; t += 512) {                        // eight on their way at a time
-            float2 p[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = t + 64 * i < tiles ? partial[(int64_t)k * ld_partial + t + 64 * i] : make_float2(-__builtin_inff(), 0.f);
-            float m = top;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i].x);
-            const float base = m == -__builtin_inff() ? 0.f : m;
-            sum *= xe_exp(top - base);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += p[i].y * xe_exp(p[i].x - base);
-            top = m;
-        }
-        const float most = wave_max(top), base = most == -__builtin_inff() ? 0.f : most;
-        sum = wave_sum(sum * xe_exp(top - base));
+        const float2 s = xe_join(partial + (int64_t)k * ld_partial, tiles, lane);
         if (lane == 0) {
-            const float l = logf(sum), v = most + l, f = l + (most - z_label[k]);
+            const float l = logf(s.y), v = s.x + l, f = l + (s.x - z_label[k]);
             const int i = rows[k];
             if (lse) lse[i] = v;
             if (loss) loss[i] = f;
@@ -1456,6 +1490,11 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         p.loss = forward ? c.loss : nullptr; p.lse = forward ? c.lse : nullptr;
         pack = p;
     }
+    // A loss of few bf16 rows in whole stages at 16-byte places is bound by W's read and by its launches: its product reads the features
+    // where they lie, every row's, and no launch packs them first (one row, 32000 x 2048: 24.5 us, 29.0 packed; 24, 65536 x 4096: 109 and 116;
+    // 64, 32000 x 1024: 23.2 and 27.0; one, 1000 x 512: 10.9 and 14.2)
+    const bool in_place = !grads && direct && c.w_bf16 && !l.kept && c.n > 0 && c.n <= 64 && c.D % 64 == 0 && ((uintptr_t)c.a % 16) == 0 &&
+                          c.lda % 8 == 0 && c.lda < (1 << 22);
     if (c.n > kXeFewRows) hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, pack);
 
     // W's rows first .. first + n - 1 as an operand; the first call packs the features as well
@@ -1465,6 +1504,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
         const bool rows_too = there < 0;
         if (direct) {
             *w = Words{(const bf16_t*)((const char*)c.W + (size_t)first * c.ldw * (c.w_bf16 ? 2 : 4)), c.ldw, 0, (int)n};
+            if (in_place) return hipSuccess;
             if (rows_too && c.a_bf16) hipLaunchKernelGGL(xent_pack_rows_kernel<bf16_t>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, pack);
             if (rows_too && !c.a_bf16) hipLaunchKernelGGL(xent_pack_rows_kernel<float>, dim3((uint32_t)l.n_padded), dim3(256), 0, s, pack);
             there = 0;
@@ -1499,6 +1539,10 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     scores.label = label; scores.ld_partial = (int)l.ld_partial;
     scores.z_label = (float*)(ws + l.z_label);
     scores.lse = lse; scores.g = g;
+    if (in_place) {
+        scores.y = (const bf16_t*)c.a; scores.ldy = c.lda; scores.y_rows = (int)c.n;
+        scores.count = nullptr; scores.label = c.y;
+    }
     auto scores_of = [&](int64_t first, int64_t n, const Words& w) {
         scores.x = w.p; scores.ldx = w.ld; scores.x_plane = w.plane; scores.x_rows = w.rows;
         scores.M = (int)n; scores.first_word = (int)first;
@@ -1557,6 +1601,11 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             if (e != hipSuccess) return e;
             const int tile_m = l.raw ? kXeRawWords : kXeTileM[l.scores.tile];
             tiles += (int)((n + tile_m - 1) / tile_m);
+        }
+        if (in_place) {
+            hipLaunchKernelGGL(xent_in_place_loss_kernel, dim3(1), dim3(1024), 0, s, pack, (const float2*)(ws + l.partial), tiles, (int)l.ld_partial,
+                               (const float*)(ws + l.z_label), c.loss, c.lse, c.total);
+            return hipGetLastError();
         }
         // (64 rows are four a wavefront of one workgroup, which then needs no launch behind it for the total)
         const bool alone = n_some <= 64;

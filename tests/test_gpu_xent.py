@@ -445,3 +445,46 @@ def test_loss_of_few_rows_with_fp32_words(n, J, D, pad, dtype):
     head.loss(W, a, y, **o, weight=weight, mean=True)
     head.sync()
     _check(o, _formula(W, a, y, weight, mean=True), dtype, "f32", D, f"{n} {J} {D}")
+
+
+@pytest.mark.parametrize("n,J,D,pad,padded", [(1, 9000, 2048, 0, 0.0), (1, 300, 64, 0, 1.0), (7, 131, 128, 8, 0.4), (32, 40000, 1024, 0, 0.2),
+                                              (33, 9001, 1984, 64, 0.5), (64, 2, 64, 0, 0.3), (64, 20000, 2048, 8, 1.0), (64, 8191, 704, 0, 0.0)])
+def test_loss_of_few_rows_where_they_lie(n, J, D, pad, padded):
+    """Features in bf16 at 16-byte places, whole stages: read in place, NaN in rows that take no part."""
+    for weighted, mean in ((False, True), (True, False)):
+        _run(n, J, D, "bf16", "bf16", seed=41, pad=pad, padded=padded, weighted=weighted, mean=mean, scale=0.75, two=True)
+        _run(n, J, D, "bf16", "bf16", seed=41, pad=pad, padded=padded, weighted=weighted, mean=mean, rows=n + 100, ws=0.0, two=True)
+
+
+def test_loss_of_few_rows_in_a_graph_with_other_labels():
+    """Each replay of a captured loss follows the labels and features that are there then; labels as far out as their type goes."""
+    import paper_1511_08486_amd as sfb
+    n, J, D = 19, 5003, 256
+    W, a, y = _inputs(n, J, D, "bf16", "bf16", seed=43)
+    s = torch.cuda.Stream()
+    head = sfb.SoftmaxHead(J, D, n, gradients=False, stream=s.cuda_stream)
+    weight = torch.rand(n, device=DEV) + 0.1
+    loss, lse, total = torch.full((n,), 77.0, device=DEV), torch.full((n,), 77.0, device=DEV), torch.full((1,), 77.0, device=DEV)
+    call = lambda: head.loss(W, a, y, loss=loss, lse=lse, total=total, weight=weight, mean=True)  # noqa: E731
+    torch.cuda.synchronize()
+    call()
+    head.sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call()
+    for i, out in enumerate(([], [0, 5], [0, 1, 2, 18], list(range(n)), [7])):
+        y.copy_(torch.randint(0, J, (n,), generator=torch.Generator().manual_seed(50 + i), dtype=torch.int32))
+        a.copy_(torch.randn(n, D, generator=torch.Generator().manual_seed(60 + i)))
+        for k, r in enumerate(out):
+            y[r] = (-2 ** 31, 2 ** 31 - 1, -1, J)[k % 4]
+            a[r] = (float("nan"), float("inf"), -float("inf"), 3e38)[k % 4]
+        for x in (loss, lse, total):
+            x.fill_(77.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(dict(loss=loss, lse=lse, total=total), _formula(W, a, y, weight, mean=True), "bf16", "bf16", D, f"replay {i}")
+        first = [x.clone() for x in (loss, lse, total)]
+        call()
+        head.sync()
+        assert all(torch.equal(p, q) for p, q in zip(first, (loss, lse, total)))
