@@ -312,7 +312,8 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
  *   loss, lse, total, weight   DEVICE fp32, NULL: not wanted (lse is needed by sfb_xent_gradients, which reads what sfb_xent_loss left)
  *   ws          DEVICE, 256-byte aligned; it belongs to the call until that has run: calls that may overlap in time, replays of captured
  *               ones included, need one each.  sfb_xent_workspace_bytes: the least a call on up to P*B rows can take, and as much as
- *               speeds it up (pieces of some 512 MB).  grads != 0: of the calls that form gradients.
+ *               speeds it up: besides what grows with P*B, U's pieces of up to 512 MB, W's terms of up to 1 GB (up to 768 MB in all where
+ *               they are only for rows of W that do not lie at 16-byte places), kept scores.  grads != 0: of the calls that form gradients.
  * sfb_xent_gradients and sfb_xent_loss_and_gradients give the same gradients, to rounding.  Results do not depend on the order in which
  * anything runs.  No two of the arrays may overlap.
  * SFB_EINVAL: a null pointer that is needed or one not aligned to its type (ws: 256), a scale that is not finite; SFB_ESHAPE: a leading dimension shorter than a row, n outside

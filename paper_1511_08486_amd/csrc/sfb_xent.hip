@@ -1294,6 +1294,7 @@ static int pair_count(int x_terms, int y_terms, int most) {
 namespace {
 constexpr int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 constexpr size_t kXePieceBytes = (size_t)512 << 20, kXeScoreBytes = (size_t)256 << 20, kXeWordBytes = (size_t)1 << 30;   // of U, kept scores and W's terms
+constexpr size_t kXePackedBytes = (size_t)768 << 20;                     // of a workspace, for the sake of W's terms where W may be read as it is
 
 // What a call does and where it keeps it.
 struct Layout {
@@ -1442,15 +1443,19 @@ size_t xent_workspace(const XentCall& c, bool grads, bool least) {
         if (b > m) m = b;
     }
     if (least) return m;
-    if (!grads && !c.w_bf16 && c.n <= 64 && c.D % 4 == 0 && c.D >= 64) { // fp32 W read as it is; pieces for rows that lie otherwise
-        const int64_t whole = up(c.J, 256);
-        const size_t b = layout_of(c, true, false, false, whole).bytes, o = layout_of(c, false, false, false, whole < 8192 ? whole : 8192).bytes;
-        return b > m ? (b > o ? b : o) : (m > o ? m : o);
-    }
-    for (int f = 0; f < 2; ++f) {
-        const size_t b = plan_call(c, direct, f != 0, grads, ~(size_t)0).bytes;
-        if (b > m) m = b;
-    }
+    // Whether W can be read as it is its address and leading dimension say, call by call: room for both ways.  Packed rows of it take as much as W
+    // itself where they are all there at once, so this way's room ends at kXePackedBytes (65536 x 4096, rows at odd places, 24 rows: loss 764
+    // us with what the other way takes, 19 pieces, and 326 in one; with gradients 2305 and 636).
+    const bool as_is = direct || (!c.w_bf16 && !grads && c.n <= 64 && c.D % 4 == 0 && c.D >= 64);
+    for (int g = 0; g <= (grads ? 1 : 0); ++g)
+        for (int f = g ? 0 : 1; f < 2; ++f) {
+            if (as_is) {
+                const size_t b = plan_call(c, true, f != 0, g != 0, ~(size_t)0).bytes;
+                if (b > m) m = b;
+            }
+            const size_t b = plan_call(c, false, f != 0, g != 0, as_is ? (m > kXePackedBytes ? m : kXePackedBytes) : ~(size_t)0).bytes;
+            if (b > m) m = b;
+        }
     return m;
 }
 

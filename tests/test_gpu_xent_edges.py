@@ -1,0 +1,31 @@
+"""Calls of the softmax head where plans change: workspaces, places of W, tiles; against the formulas in 64 bits."""
+import pytest
+import torch
+
+from test_gpu_xent import DEV, PAIRS, TYPES, _check, _formula, _inputs, _run
+
+pytestmark = pytest.mark.gpu
+
+
+def _loss(W, a, y, dtype, w_dtype, rows=None, weight=None, least=False):
+    """loss, lse and total of a head that forms no gradients, on a workspace of NaN"""
+    import paper_1511_08486_amd as sfb
+    (J, D), n = W.shape, a.shape[0]
+    head = sfb.SoftmaxHead(J, D, rows or n, dtype=dtype, w_dtype=w_dtype, gradients=False)
+    if least:
+        head = sfb.SoftmaxHead(J, D, rows or n, dtype=dtype, w_dtype=w_dtype, gradients=False, workspace_bytes=head.least_bytes)
+        assert head._ws.numel() == max(head.least_bytes, 256)
+    head._ws.fill_(255)
+    o = dict(loss=torch.full((n,), 7.0, device=DEV), lse=torch.full((n,), 7.0, device=DEV), total=torch.zeros(1, device=DEV))
+    head.loss(W, a, y, **o, weight=weight, mean=True)
+    head.sync()
+    return o
+
+
+@pytest.mark.parametrize("n,J,D,pad,offset", [(1, 9000, 136, 1, 0), (24, 9000, 136, 3, 0), (64, 600, 1600, 1, 0), (33, 5000, 72, 0, 1), (70, 9000, 136, 1, 0),
+                                              (200, 3000, 1608, 5, 3)])
+def test_loss_alone_with_bf16_words_at_odd_places(n, J, D, pad, offset):
+    """D % 8 = 0, so that W could be read as it is at other places; a head without gradients, whose best workspace is small then."""
+    W, a, y = _inputs(n, J, D, "bf16", "bf16", 70 + n, pad=pad, offset=offset, padded=0.2 if n > 1 else 0.0)
+    for least in (False, True):
+        _check(_loss(W, a, y, "bf16", "bf16", least=least), _formula(W, a, y, mean=True), "bf16", "bf16", D, f"{n} {J} {D} least {least}")

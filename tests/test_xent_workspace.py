@@ -1,0 +1,33 @@
+"""How much workspace a head of given sizes is told to take, on the host."""
+import ctypes as C
+
+import pytest
+
+
+def _bytes(J, D, rows, dtype, w_dtype, grads):
+    from paper_1511_08486_amd import binding as b
+    types = {"f32": b.SFB_F32, "bf16": b.SFB_BF16}
+    c, least, best = C.c_void_p(), C.c_size_t(), C.c_size_t()
+    assert b.lib.sfb_create(C.byref(c), b.SFB_MLR, J, D, 1, rows, types[dtype], None) == 0
+    try:
+        assert b.lib.sfb_xent_workspace_bytes(c, types[w_dtype], grads, C.byref(least), C.byref(best)) == 0
+    finally:
+        b.lib.sfb_destroy(c)
+    return least.value, best.value
+
+
+@pytest.mark.parametrize("J,D,rows,grads", [(32000, 2048, 1, 0), (131072, 4096, 1, 0), (131072, 2048, 2000, 0), (65536, 4096, 24, 0), (65536, 4096, 24, 1),
+                                            (32000, 2048, 1, 1), (1000, 8192, 24, 0), (1000, 8192, 24, 1), (500, 64, 7, 0)])
+def test_bf16_words_that_do_not_lie_at_16_byte_places_have_room(J, D, rows, grads):
+    """Where W lies is known call by call: the best workspace holds the terms of as many words as fill the card, or of all (the least: 256)."""
+    least, best = _bytes(J, D, rows, "bf16", "bf16", grads)
+    words = min(J, 32768)
+    assert best - least >= max(0, words - 256) * D * 2
+
+
+@pytest.mark.parametrize("J,D,rows", [(1000, 1024, 1), (4000, 4096, 64), (8000, 2048, 24)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_fp32_words_have_room_for_their_terms_and_scores(J, D, rows, dtype):
+    """A loss of few rows: two fp16 terms of all of W, and a plane of the scores."""
+    least, best = _bytes(J, D, rows, dtype, "f32", 0)
+    assert best - least >= (J - 256) * D * 4 + J * 64 * 4
