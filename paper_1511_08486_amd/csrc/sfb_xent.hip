@@ -1308,11 +1308,20 @@ struct Layout {
 };
 }  // namespace
 
+// Whether fp32 words read as they are give the loss of few rows sooner than their terms do.  Reading them takes a stage's latency after another, its
+// workgroups have all of D; terms cost W two more passes at 5.4 TB/s and 4 us, and their product is cut into slices of D.  One row of
+// bf16, as they are and as terms: 1000 x 1024 27 us and 16, 1000 x 8192 146 and 41, 4000 x 2048 44 and 34, 8000 x 4096 78 and 78, 16000 x 2048 45
+// and 72, 16000 x 8192 164 and 371; 64 rows of fp32: 1000 x 4096 120 and 33, 16000 x 4096 134 and 250.  The choice loses 16 % at most there.
+static bool raw_pays(const XentCall& c) {
+    const double stage_us = c.a_bf16 ? (c.n > 32 ? 1.20 : 1.06) : (c.n > 32 ? 1.63 : 1.23);
+    return stage_us * (double)((c.D + 63) / 64) <= 4.0 + 2.2e-6 * (double)c.J * (double)c.D;
+}
+
 // Rows of W that a product reads as they are: in bf16 with bf16 features; in fp32 for the loss of few rows.  Pieces of 16 bytes, 32-bit offsets.
 static bool reads_w_directly(const XentCall& c, bool grads) {
     if (c.D < 64 || ((uintptr_t)c.W % 16) != 0 || c.ldw >= (1 << 22)) return false;
     if (c.w_bf16) return c.a_bf16 && c.D % 8 == 0 && c.ldw % 8 == 0;
-    return !grads && c.n <= 64 && c.D % 4 == 0 && c.ldw % 4 == 0;
+    return !grads && c.n <= 64 && c.D % 4 == 0 && c.ldw % 4 == 0 && raw_pays(c);
 }
 
 // piece: words of a piece, a multiple of 256

@@ -29,3 +29,27 @@ def test_loss_alone_with_bf16_words_at_odd_places(n, J, D, pad, offset):
     W, a, y = _inputs(n, J, D, "bf16", "bf16", 70 + n, pad=pad, offset=offset, padded=0.2 if n > 1 else 0.0)
     for least in (False, True):
         _check(_loss(W, a, y, "bf16", "bf16", least=least), _formula(W, a, y, mean=True), "bf16", "bf16", D, f"{n} {J} {D} least {least}")
+
+
+def _product(head):
+    """The kernel that the head's last call multiplied with first."""
+    import ctypes as C
+    from paper_1511_08486_amd import binding as b
+    name = C.create_string_buffer(200)
+    assert b.lib.sfb_last_kernel(head._ctx, 8, name, 200, None) == 0
+    return name.value.decode()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 64])
+def test_few_fp32_words_of_long_rows_are_cut_into_slices_of_features(n, dtype):
+    """1000 words are eight workgroups where W is read as it is; more words of shorter rows fill the card that way."""
+    import paper_1511_08486_amd as sfb
+    for J, D, as_it_is in ((1000, 8192, False), (24000, 512, True)):
+        W, a, y = _inputs(n, J, D, dtype, "f32", 80)
+        head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype="f32", gradients=False)
+        loss = torch.empty(n, device=DEV)
+        head.loss(W, a, y, loss=loss)
+        head.sync()
+        assert ("raw" in _product(head)) == as_it_is, _product(head)
+        _check(dict(loss=loss), _formula(W, a, y), dtype, "f32", D, f"{n} {J} {D}")
