@@ -1401,20 +1401,28 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
 // Whether a call keeps its scores: they fit, and forming them again (or leaving most compute units idle) would take longer than their
 // way to memory and back.  A score costs 2 D flops a pair of terms again, at about 1.1 PFLOP/s, or some 12 bytes at 4 TB/s.
 // Measured, kept and not, bf16: both directions, 32 rows, 65536 x 4096: 450 us and 532; 64 rows, 1000 x 2048: 35 and 71; one, 32000 x 1504:
-// 88 and 95.  The loss alone splits k over idle units: 64 rows, 8000 x 4096: 32 and 50; one, 1000 x 4096: 16 and 31; where it gains least
-// (one row, 8000 x 1504) the pass over the scores costs more than that: 22 and 19.
-static bool keeps_scores(const XentCall& c, bool forward, bool grads) {
+// 88 and 95.  The loss alone splits k over idle units, so that its stages (0.33 to 0.45 us each, one after another) are fewer, and pays a
+// launch, the slices' planes and less of a tile's reuse for it: 7 us (3 where a packing launch goes before either way) and W's terms at 4.2 TB/s
+// fit what was measured up to 64 rows.  One row, 1000 x 4096: 16 and 27, 4000 x 2048 16 and 17, 4000 x 1504 15 and 18, 8000 x 1504 20 and 18, 8000 x
+// 4096 31 and 28, 8000 x 8192 41 and 48; 64 rows, 8000 x 1536 24 and 24, 8000 x 4096 32 and 44.  The choice loses a tenth at most there.
+static bool keeps_scores(const XentCall& c, bool direct, bool forward, bool grads) {
     const int64_t n = c.n > 0 ? c.n : 1, whole = up(c.J, 256);
     if ((size_t)up(n, 256) * whole * 4 > kXeScoreBytes) return false;
     const int pairs = c.a_bf16 && c.w_bf16 ? 1 : c.a_bf16 || c.w_bf16 ? 2 : 3;
     const int64_t tiles = ((c.J + 127) / 128) * ((n + 127) / 128);
-    return c.D * pairs >= 1500 && ((forward && grads) || tiles < (n > 64 ? 200 : 64));
+    if (c.D * pairs < 1500) return false;
+    if (!grads && n <= 64) {
+        const double stages = (double)((c.D + 63) / 64) * pairs, w_bytes = (double)c.J * (double)c.D * (c.w_bf16 ? 2.0 : 4.0);
+        const double gain = stages * (n > 32 ? 0.45 : pairs == 1 ? 0.33 : 0.39), cost = (direct && c.D % 64 == 0 ? 7.0 : 3.0) - (n > 32 ? 2.0 : 0.0) + w_bytes / 4.2e6;
+        return tiles < 64 && gain > cost;
+    }
+    return (forward && grads) || tiles < (n > 64 ? 200 : 64);
 }
 
 // The layout that a call on c's sizes takes within `bytes`; .bytes > bytes: there is none
 static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads, size_t bytes) {
     const int64_t whole = up(c.J, 256) / 256;
-    for (int kept = !(direct && !c.w_bf16) && keeps_scores(c, forward, grads); kept >= 0; --kept) {
+    for (int kept = !(direct && !c.w_bf16) && keeps_scores(c, direct, forward, grads); kept >= 0; --kept) {
         if (!grads && direct) {
             const Layout l = layout_of(c, true, false, kept != 0, whole * 256);
             if (l.bytes <= bytes || !kept) return l;

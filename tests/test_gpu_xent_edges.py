@@ -53,3 +53,18 @@ def test_few_fp32_words_of_long_rows_are_cut_into_slices_of_features(n, dtype):
         head.sync()
         assert ("raw" in _product(head)) == as_it_is, _product(head)
         _check(dict(loss=loss), _formula(W, a, y), dtype, "f32", D, f"{n} {J} {D}")
+
+
+@pytest.mark.parametrize("n,J,D,sliced", [(1, 8000, 1504, False), (1, 8000, 4096, False), (1, 1000, 4096, True), (64, 8000, 4096, True), (1, 500, 1024, False)])
+def test_the_loss_alone_is_cut_into_slices_where_that_gains(n, J, D, sliced):
+    import ctypes as C
+    import paper_1511_08486_amd as sfb
+    from paper_1511_08486_amd import binding as b
+    W, a, y = _inputs(n, J, D, "bf16", "bf16", 81)
+    head = sfb.SoftmaxHead(J, D, n, gradients=False)
+    loss, grid = torch.empty(n, device=DEV), C.c_int32()
+    head.loss(W, a, y, loss=loss)
+    head.sync()
+    assert b.lib.sfb_last_kernel(head._ctx, 8, None, 0, C.byref(grid)) == 0
+    assert (grid.value > (J + 127) // 128) == sliced, grid.value         # tiles of 128 words at least: more workgroups are slices
+    _check(dict(loss=loss), _formula(W, a, y), "bf16", "bf16", D, f"{n} {J} {D}")
