@@ -18,7 +18,7 @@
 //                  are in U, and U's rows are divided by what their weight bounds them by.  A bf16 dA takes one term of each (2^-12).
 //   dW             three bf16 terms (exact) and six products (three with bf16 features): along its contraction, the rows, the factors of a
 //                  rare word may all be below 2^-40 of a label's, and must not be rounded by that.
-// Small problems keep their scores (256 MB at most) where forming them again would take longer than reading them.
+// Small problems keep their scores (256 MB at most, their slices of D included) where forming them again would take longer than reading them.
 //
 // Bound by: many rows, the matrix cores at the clock that they hold (131072 words, 4096 rows and features, bf16: scores 1.20 PFLOP/s, with U
 // 1.10, dA 1.30, dW 1.18, the clock at 1.63 GHz, 64 to 75 % of its cycles in matrix instructions, LDS a fifth, no bank conflicts); few rows, W's
@@ -1354,7 +1354,9 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     }
     const int score_pairs = l.f16 ? pair_count(l.w16_terms, l.a16_terms, 1) : 1;
     const int64_t row_tiles = (n + 63) / 64, word_tiles = (words + 63) / 64;
-    l.scores = tiling_for(words, n, (int64_t)l.k_tiles * score_pairs, kept ? 16 : 1, true, false,
+    l.ld_z = up(c.J, 256);
+    const int64_t planes = (int64_t)(kXeScoreBytes / ((size_t)l.n_padded * l.ld_z * 4)), slices = !kept || planes < 1 ? 1 : planes < 16 ? planes : 16;
+    l.scores = tiling_for(words, n, (int64_t)l.k_tiles * score_pairs, slices, true, false,
                           kept ? kXeStore : grads ? kXeU : kXeStats, kept ? 4.0 : 2.0 * (l.u_terms + l.u16_terms));
     if (grads) {
         l.dA = tiling_for(c.D, n, word_tiles * (l.f16 ? pair_count(l.w16_terms, l.u16_terms, l.dA_most) : 1), 64, true, true, kXeStore, 4.0);
@@ -1384,7 +1386,6 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
         l.a16 = take((size_t)l.a16_terms * l.n_padded * l.ld_k * 2);
     }
     if (l.a_terms) l.a = take((size_t)l.a_terms * l.n_padded * l.ld_a * 2);
-    l.ld_z = up(c.J, 256);
     if (kept) l.z = take((size_t)l.scores.splits * l.n_padded * l.ld_z * 4);
     l.ld_partial = up(c.J, 256) / 128;
     if (!kept) l.partial = take((size_t)l.ld_partial * n * 8);

@@ -31,3 +31,11 @@ def test_few_fp32_words_have_room_for_their_terms_and_scores(J, D, rows, dtype):
     """A loss of few rows: two fp16 terms of all of W, and a plane of the scores."""
     least, best = _bytes(J, D, rows, dtype, "f32", 0)
     assert best - least >= (J - 256) * D * 4 + J * 64 * 4
+
+
+@pytest.mark.parametrize("J,D,rows", [(117884, 6401, 512), (118441, 6401, 500)])
+def test_kept_scores_with_all_their_slices_take_256_mb_at_most(J, D, rows):
+    """Best = kept scores + U (512 MB at most) + W's terms (1 GB) + the rows' terms + dA's sums (8 slices) and the rows' and words' other values."""
+    padded, whole, features = (rows + 255) // 256 * 256, (J + 255) // 256 * 256, (D + 63) // 64 * 64
+    rest = min(5 * padded * whole * 2, 1 << 29) + min(whole * features * 4, 1 << 30) + 5 * padded * features * 2 + 8 * rows * (D + 7) * 4 + 64 * padded + 4 * whole
+    assert _bytes(J, D, rows, "f32", "f32", 1)[1] <= (256 << 20) + rest
