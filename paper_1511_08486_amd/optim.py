@@ -24,11 +24,10 @@ class _Stream:
             self._check(lib.sfb_create(C.byref(self._ctx), *shape, C.c_void_p(self.stream)), "sfb_create")
 
     def _scratch(self, nbytes):
-        """A workspace that the allocator hands to nobody else before this stream is through with it."""
-        ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
-        if self.stream != torch.cuda.current_stream(self.device).cuda_stream:
-            ws.record_stream(torch.cuda.ExternalStream(self.stream, device=self.device))
-        return ws
+        """A workspace that is this stream's own from the allocator on.  (From the current stream's memory it could be a block that was freed
+        there while what used it still waits to run.)"""
+        with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, device=self.device)):
+            return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
 
     def _check(self, status, where):
         if status != 0:

@@ -68,3 +68,28 @@ def test_the_loss_alone_is_cut_into_slices_where_that_gains(n, J, D, sliced):
     assert b.lib.sfb_last_kernel(head._ctx, 8, None, 0, C.byref(grid)) == 0
     assert (grid.value > (J + 127) // 128) == sliced, grid.value         # tiles of 128 words at least: more workgroups are slices
     _check(dict(loss=loss), _formula(W, a, y), "bf16", "bf16", D, f"{n} {J} {D}")
+
+
+def test_a_workspace_is_not_taken_from_another_streams_freed_memory():
+    """What was freed on the current stream may still be in use there: an object of another stream must not be handed it."""
+    import paper_1511_08486_amd as sfb
+    side = torch.cuda.Stream(device=DEV)
+    grads = [torch.ones(3 << 20, device=DEV)]
+    kinds = ((lambda: sfb.SoftmaxHead(9000, 520, 200, stream=side.cuda_stream)), (lambda: sfb.GradNorm(grads, stream=side.cuda_stream)))
+    for make in kinds:
+        first = make()
+        nbytes = first._ws.numel()
+        torch.cuda.synchronize()
+        freed = [torch.empty(nbytes, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        places = {t.data_ptr() for t in freed}
+        del freed
+        second = make()
+        assert second._ws.data_ptr() not in places
+        again = torch.empty(nbytes, dtype=torch.uint8, device=DEV)      # (they were there to be taken)
+        assert again.data_ptr() in places
+        with torch.cuda.stream(side):                                    # the stream's own freed memory is what it may take
+            del first
+    with torch.cuda.stream(side):                                        # and an object of the default stream made on another
+        head = sfb.SoftmaxHead(300, 64, 8, stream=0)
+        assert head.stream == 0 and head._ws.numel() >= 256
+    torch.cuda.synchronize()
