@@ -750,20 +750,6 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(const XentPack p) {
     xe_find_rows(p, -1, true, 16, &count);
 }
 
-__device__ __forceinline__ float xe_block_top(float top) {
-    __shared__ float part[4];
-    top = wave_max(top);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
-    __syncthreads();
-    return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-}
-__device__ __forceinline__ float xe_top4(f32x4 x, float top) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.f);
-    return top;
-}
-__device__ __forceinline__ int xe_row_exponent(float top) { return (int)(__float_as_uint(top) >> 23) - 127 - 14; }   // (2^-126 for all below)
-
 // A row of D elements by a workgroup of 256 threads, or by a wavefront of it (LANES = 64, rows of up to 2048): the first 4 HELD a thread stay
 // in registers between what looks them over and what takes them (long rows of a large W, all on their way at once, are out of the
 // caches by then: 10000 x 21504 in fp32 452 us with 16 elements a thread, 371 with 96).
