@@ -23,6 +23,7 @@ namespace sfb {
 
 constexpr int kAwThreads = 256, kAwPer = 8, kAwChunk = 4096;             // elements a workgroup takes
 constexpr int kAwRounds = kAwChunk / (kAwThreads * kAwPer);
+constexpr int kAwLaunch = (1 << 24) - 1;                                 // workgroups of a launch: it has fewer than 2^32 threads
 
 struct AdamwTable {
     AdamwTensor t[kAdamwTensors];
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(kAwThreads) void adamw_unpack_kernel(const AdamwTab
     }
 }
 
-// Splits the list into launches of at most kAdamwTensors tensors and 2^30 workgroups.
+// Splits the list into launches of at most kAdamwTensors tensors and kAwLaunch workgroups (2^36 elements).
 template <class Launch>
 static hipError_t aw_each_table(const AdamwTensor* t, int count, Launch launch) {
     AdamwTable table;
@@ -289,7 +290,7 @@ static hipError_t aw_each_table(const AdamwTensor* t, int count, Launch launch) 
         int64_t chunks = 0;
         for (; i < count && table.count < kAdamwTensors; ++i) {
             const int64_t c = (t[i].n + kAwChunk - 1) / kAwChunk;
-            if (chunks + c > (1 << 30) && table.count > 0) break;
+            if (chunks + c > kAwLaunch && table.count > 0) break;
             if (t[i].n > 0) {
                 table.t[table.count] = t[i];
                 table.t[table.count].first = first;
@@ -417,7 +418,7 @@ hipError_t launch_grad_norm(const GradTensor* t, int count, bool bf16, float max
         for (; i < count && table.count < kGradTensors; ++i) {
             const int64_t c = (t[i].n + kGnChunk - 1) / kGnChunk;
             if (c == 0) continue;
-            if (chunks + c > (1 << 30) && table.count > 0) break;
+            if (chunks + c > kAwLaunch && table.count > 0) break;
             table.t[table.count] = t[i];
             table.first_chunk[table.count++] = (int32_t)chunks;
             chunks += c;

@@ -1410,8 +1410,10 @@ static bool keeps_scores(const XentCall& c, bool direct, bool forward, bool grad
 static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads, size_t bytes) {
     const int64_t whole = up(c.J, 256) / 256;
     for (int kept = !(direct && !c.w_bf16) && keeps_scores(c, direct, forward, grads); kept >= 0; --kept) {
+        // a launch has fewer than 2^32 threads, 256 for 128 x 128 results: fewer than 2^38 scores a piece
+        const int64_t launch_most = (((int64_t)1 << 37) / up(c.n > 0 ? c.n : 1, 256)) / 256;
         if (!grads && direct) {
-            const Layout l = layout_of(c, true, false, kept != 0, whole * 256);
+            const Layout l = layout_of(c, true, false, kept != 0, (whole < launch_most ? whole : launch_most) * 256);
             if (l.bytes <= bytes || !kept) return l;
             continue;
         }
@@ -1421,6 +1423,7 @@ static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads
         int64_t lo = 1, hi = whole < (1 << 14) ? whole : (1 << 14);      // 32-bit offsets inside a tile: 2^22 words at most
         if (u_bytes > 0 && hi > (int64_t)(kXePieceBytes / u_bytes)) hi = (int64_t)(kXePieceBytes / u_bytes);
         if (w_bytes > 0 && hi > (int64_t)(kXeWordBytes / w_bytes)) hi = (int64_t)(kXeWordBytes / w_bytes);
+        if (hi > launch_most) hi = launch_most;
         if (hi < 1) hi = 1;
         if (layout_of(c, direct, grads, kept != 0, hi * 256).bytes <= bytes) lo = hi;    // (bytes may fall as pieces grow: fewer splits of dA)
         while (lo < hi) {

@@ -93,3 +93,21 @@ def test_a_workspace_is_not_taken_from_another_streams_freed_memory():
         head = sfb.SoftmaxHead(300, 64, 8, stream=0)
         assert head.stream == 0 and head._ws.numel() >= 256
     torch.cuda.synchronize()
+
+
+def test_loss_of_more_scores_than_a_launch_takes():
+    """2^39 scores in fp32: the vocabulary goes in pieces, whatever the workspace holds."""
+    import paper_1511_08486_amd as sfb
+    n, J, D = 1 << 20, 1 << 19, 64
+    g = torch.Generator(device=DEV).manual_seed(7)
+    W, a = torch.randn(J, D, generator=g, device=DEV) * 0.25, torch.randn(n, D, generator=g, device=DEV)
+    y = torch.randint(0, J, (n,), generator=g, device=DEV, dtype=torch.int32)
+    y[5::1000] = -1
+    loss, lse = torch.full((n,), 7.0, device=DEV), torch.full((n,), 7.0, device=DEV)
+    head = sfb.SoftmaxHead(J, D, n, dtype="f32", w_dtype="f32", gradients=False)
+    head.loss(W, a, y, loss=loss, lse=lse)
+    head.sync()
+    rows = torch.cat([torch.arange(0, 8), torch.tensor([1005]), torch.randint(0, n, (40,), generator=torch.Generator().manual_seed(1)), torch.arange(n - 8, n)]).to(DEV)
+    assert (loss[5::1000] == 0).all() and torch.isfinite(loss).all()
+    want = _formula(W, a[rows], y[rows])
+    _check(dict(loss=loss[rows], lse=lse[rows]), want, "f32", "f32", D, "rows")
