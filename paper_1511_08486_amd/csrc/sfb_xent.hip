@@ -572,39 +572,34 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
 // stages, so that two workgroups fit a compute unit (65536 x 4096, one row of bf16: 235 us, 4.6 TB/s; one workgroup with three or four stages
 // 289; its terms packed first 728), three where only one fits anyway (fp32 features: 290; packed 917).  The leading products and the others have sums of their own, the former in blocks of 256 k.
 // LDS rows of W: 256 bytes, 16-byte piece p of row r at p ^ (r & 15).
+// ANY: rows of W at any 4-byte place and of any length.  They come through registers, two stages ahead, since LDS-DMA wants whole pieces at
+// 16-byte places; what lies behind a row is not read (65536 x 4096, rows 4097 apart: one row of bf16 199 us, 64 of fp32 289; their terms packed
+// first 607 and 733).
 constexpr int kXeRawWords = 128;
-template <int NT, int TERMS> constexpr int kXeRawStages = TERMS == 3 && NT == 1 ? 3 : 2;
+template <int NT, int TERMS, bool ANY> constexpr int kXeRawStages = TERMS == 3 && NT == 1 && !ANY ? 3 : 2;
 
-template <int NT, int TERMS>
-__global__ __launch_bounds__(256, 1) void xent_raw_scores_kernel(const XentProduct a) {
-    constexpr int X_BYTES = kXeRawWords * 256, Y_BYTES = NT * 32 * 128, STAGE = X_BYTES + TERMS * Y_BYTES, LOADS = 8 + TERMS * NT, ST = kXeRawStages<NT, TERMS>;
+template <int NT, int TERMS, bool ANY>
+__global__ __launch_bounds__(256, ANY && TERMS == 1 ? 2 : 1) void xent_raw_scores_kernel(const XentProduct a) {
+    constexpr int X_BYTES = kXeRawWords * 256, Y_BYTES = NT * 32 * 128, STAGE = X_BYTES + TERMS * Y_BYTES, LOADS = 8 + TERMS * NT, ST = kXeRawStages<NT, TERMS, ANY>;
     extern __shared__ __attribute__((aligned(16))) unsigned char xe_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5, m0 = blockIdx.x * kXeRawWords, count = *a.count;
     if (count == 0) return;
     const float* const W = reinterpret_cast<const float*>(a.x) + (int64_t)m0 * a.ldx;
-    uint32_t x_off[8], y_off[NT];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {                                        // 16 rows of W an access of the four wavefronts
-        const int in16 = wave * 4 + (lane >> 4), r = min(m0 + i * 16 + in16, a.x_rows - 1) - m0;
-        x_off[i] = (uint32_t)r * (uint32_t)a.ldx * 4u + (uint32_t)(((lane & 15) ^ in16) * 16);
-    }
+    const int in16 = wave * 4 + (lane >> 4);                             // 16 rows of W an access of the four wavefronts
+    uint32_t y_off[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
         y_off[i] = (uint32_t)((i * 4 + wave) * 8 + (lane >> 3)) * (uint32_t)a.ldy * 2u + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7) ^ (wave & 1)) * 16);
     const uint32_t lds0 = xe_lds_address(xe_lds);
     const int stages = a.k_tiles;
-    auto request = [&](int s) {
-        const bool last = s == stages - 1;
-        const uint32_t to = lds0 + (s % ST) * STAGE;
-        const float* const x = W + (last ? a.last_x : s * kXeK);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) xe_dma(x, x_off[i], to + (i * 4 + wave) * 1024);
+    auto request_y = [&](int s) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + (s % ST) * STAGE + X_BYTES;
 #pragma unroll
         for (int t = 0; t < TERMS; ++t) {
-            const bf16_t* const y = a.y + t * a.y_plane + (last ? a.last_y : s * kXeK);
+            const bf16_t* const y = a.y + t * a.y_plane + (s == stages - 1 ? a.last_y : s * kXeK);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) xe_dma(y, y_off[i], to + X_BYTES + t * Y_BYTES + (i * 4 + wave) * 1024);
+            for (int i = 0; i < NT; ++i) xe_dma(y, y_off[i], to + t * Y_BYTES + (i * 4 + wave) * 1024);
         }
     };
     f32x16 acc[1][NT], sum[NT], small[NT];
@@ -612,11 +607,8 @@ __global__ __launch_bounds__(256, 1) void xent_raw_scores_kernel(const XentProdu
     for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[0][j][e] = sum[j][e] = small[j][e] = 0.f;
-    for (int s = 0; s < min(ST - 1, stages); ++s) request(s);
-    for (int s = 0; s < stages; ++s) {
-        if (s + 1 < stages) xe_stage_barrier<(ST - 2) * LOADS>();        // this stage is there, the next of three may be on its way
-        else xe_wait_barrier();
-        if (s + ST - 1 < stages) request(s + ST - 1);                    // into the buffer that everybody is through with
+    // the products of stage s, which is in LDS
+    auto multiply = [&](int s) __attribute__((always_inline)) {
         const unsigned char* const now = xe_lds + (s % ST) * STAGE;
         const unsigned char* const w_row = now + (wave * 32 + l32) * 256;
         split_for<0, 4>([&](auto sc) {
@@ -659,6 +651,86 @@ __global__ __launch_bounds__(256, 1) void xent_raw_scores_kernel(const XentProdu
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[0][j][e] = 0.f;
             }
+        }
+    };
+    if constexpr (ANY) {
+        const int k = 4 * (lane & 15), features = a.x_cols, full = stages - 1;
+        const float* row[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = W + (int64_t)(min(m0 + i * 16 + in16, a.x_rows - 1) - m0) * a.ldx + k;
+        f32x4 even[8], odd[8];                                           // stages on their way
+        auto load = [&](int s, f32x4 (&w)[8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const sp_f32x4u*>(row[i] + s * kXeK);
+        };
+        auto put = [&](int s, const f32x4 (&w)[8]) __attribute__((always_inline)) {
+            unsigned char* const to = xe_lds + (s % ST) * STAGE;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<f32x4*>(to + (i * 16 + in16) * 256 + (((lane & 15) ^ in16) << 4)) = w[i];
+        };
+        // The eight loads of stage s + 1 were requested after stage s and its features: eight on their way leave nothing of that.  A stage's buffer is
+        // free at the barrier: everybody is through with the stage before
+        auto step = [&](int s, f32x4 (&w)[8]) __attribute__((always_inline)) {
+            put(s, w);
+            xe_stage_barrier<8>();
+            request_y(s + 1);
+            load(s + 2, w);
+            asm volatile("" ::: "memory");                               // (the loads stay in front)
+            multiply(s);
+        };
+        request_y(0);
+        int s = 0;
+        if (full > 3) {                                                  // (no branch among the loads: waits are counted)
+            load(0, even);
+            asm volatile("" ::: "memory");                               // in this order
+            load(1, odd);
+            do {
+                step(s, even);
+                step(s + 1, odd);
+                s += 2;
+            } while (s + 3 < full);
+        } else {
+            if (full > 0) load(0, even);
+            if (full > 1) load(1, odd);
+        }
+        for (; s < full; ++s) {                                          // the last three at most
+            put(s, even);
+            xe_wait_barrier();
+            request_y(s + 1);
+            multiply(s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) even[i] = odd[i];
+            if (s + 2 < full) load(s + 2, odd);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)                                      // a row may end anywhere in the last stage
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = full * kXeK + e, inside = min(at + k, features - 1) - k;
+                even[i][e] = row[i][inside];
+                if (at + k >= features) even[i][e] = 0.f;
+            }
+        put(full, even);
+        xe_wait_barrier();
+        multiply(full);
+    } else {
+        uint32_t x_off[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x_off[i] = (uint32_t)(min(m0 + i * 16 + in16, a.x_rows - 1) - m0) * (uint32_t)a.ldx * 4u + (uint32_t)(((lane & 15) ^ in16) * 16);
+        auto request = [&](int s) {
+            const uint32_t to = lds0 + (s % ST) * STAGE;
+            const float* const x = W + (s == stages - 1 ? a.last_x : s * kXeK);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xe_dma(x, x_off[i], to + (i * 4 + wave) * 1024);
+            request_y(s);
+        };
+        for (int s = 0; s < min(ST - 1, stages); ++s) request(s);
+        for (int s = 0; s < stages; ++s) {
+            if (s + 1 < stages) xe_stage_barrier<(ST - 2) * LOADS>();    // this stage is there, the next of three may be on its way
+            else xe_wait_barrier();
+            if (s + ST - 1 < stages) request(s + ST - 1);                // into the buffer that everybody is through with
+            multiply(s);
         }
     }
     xe_wait_barrier();
@@ -1181,15 +1253,20 @@ static hipError_t raise_lds(K* kernel, size_t lds, std::atomic<uint64_t>& raised
     return hipSuccess;
 }
 
-template <int NT, int TERMS>
+template <int NT, int TERMS, bool ANY>
 static hipError_t launch_raw_scores(const XentProduct& a, hipStream_t s) {
-    constexpr size_t lds = (size_t)kXeRawStages<NT, TERMS> * (kXeRawWords * 256 + TERMS * NT * 32 * 128);
+    constexpr size_t lds = (size_t)kXeRawStages<NT, TERMS, ANY> * (kXeRawWords * 256 + TERMS * NT * 32 * 128);
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> raised{0};
-    const hipError_t e = raise_lds(&xent_raw_scores_kernel<NT, TERMS>, lds, raised);
+    const hipError_t e = raise_lds(&xent_raw_scores_kernel<NT, TERMS, ANY>, lds, raised);
     if (e != hipSuccess) return e;
-    SFB_LAUNCH((xent_raw_scores_kernel<NT, TERMS>), dim3((uint32_t)((a.M + kXeRawWords - 1) / kXeRawWords)), dim3(256), lds, s, a);
+    SFB_LAUNCH((xent_raw_scores_kernel<NT, TERMS, ANY>), dim3((uint32_t)((a.M + kXeRawWords - 1) / kXeRawWords)), dim3(256), lds, s, a);
     return hipGetLastError();
+}
+template <bool ANY>
+static hipError_t launch_raw_scores(const XentProduct& a, bool a_bf16, int rows, hipStream_t s) {
+    if (a_bf16) return rows > 32 ? launch_raw_scores<2, 1, ANY>(a, s) : launch_raw_scores<1, 1, ANY>(a, s);
+    return rows > 32 ? launch_raw_scores<2, 3, ANY>(a, s) : launch_raw_scores<1, 3, ANY>(a, s);
 }
 
 // Tiles, m x n; kXe128x128Lone: four stages on their way instead of two, a compute unit to itself.
@@ -1285,7 +1362,8 @@ constexpr size_t kXePackedBytes = (size_t)768 << 20;                     // of a
 // What a call does and where it keeps it.
 struct Layout {
     int64_t n_padded, piece, ld_k, ld_a, ld_acc, ld_z, ld_partial; // piece: words; ld_k: features to whole stages
-    bool f16, direct, kept, raw;                       // fp16 terms (either operand fp32); W read as it is; scores of all words kept; fp32 W as it is
+    bool f16, direct, kept, raw, raw_any;              // fp16 terms (either operand fp32); W read as it is; scores of all words kept; fp32 W as it
+                                                       // is, and at any place
     int k_tiles, window;
     int a_terms, a16_terms, w16_terms, u_terms, u16_terms;
     int score_most, dA_most, dW_most;                  // pairs of terms
@@ -1303,11 +1381,15 @@ static bool raw_pays(const XentCall& c) {
     return stage_us * (double)((c.D + 63) / 64) <= 4.0 + 2.2e-6 * (double)c.J * (double)c.D;
 }
 
-// Rows of W that a product reads as they are: in bf16 with bf16 features; in fp32 for the loss of few rows.  Pieces of 16 bytes, 32-bit offsets.
+// Rows of W that LDS-DMA takes: pieces of 16 bytes, 32-bit offsets
+static bool words_in_pieces(const XentCall& c) {
+    const int per = c.w_bf16 ? 8 : 4;
+    return c.D >= 64 && c.D % per == 0 && c.ldw % per == 0 && ((uintptr_t)c.W % 16) == 0 && c.ldw < (1 << 22);
+}
+// Rows of W that a product reads as they are: in bf16 with bf16 features, in pieces; in fp32 for the loss of few rows.
 static bool reads_w_directly(const XentCall& c, bool grads) {
-    if (c.D < 64 || ((uintptr_t)c.W % 16) != 0 || c.ldw >= (1 << 22)) return false;
-    if (c.w_bf16) return c.a_bf16 && c.D % 8 == 0 && c.ldw % 8 == 0;
-    return !grads && c.n <= 64 && c.D % 4 == 0 && c.ldw % 4 == 0 && raw_pays(c);
+    if (c.w_bf16) return c.a_bf16 && words_in_pieces(c);
+    return !grads && c.n <= 64 && raw_pays(c);
 }
 
 // piece: words of a piece, a multiple of 256
@@ -1315,6 +1397,7 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     Layout l{};
     const int64_t n = c.n > 0 ? c.n : 1, words = piece < c.J ? piece : c.J;
     l.raw = direct && !c.w_bf16;
+    l.raw_any = l.raw && !words_in_pieces(c);
     l.f16 = !l.raw && !(c.a_bf16 && c.w_bf16);
     l.direct = direct;
     l.kept = kept;
@@ -1322,7 +1405,7 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
     l.n_padded = n <= 64 ? 64 : n <= 128 ? 128 : up(n, 256);             // whole tiles, and whole stages of dW's k
     l.k_tiles = (int)((c.D + 63) / 64);
     l.ld_k = 64 * (int64_t)l.k_tiles;
-    l.window = direct && c.D % 64 != 0 ? (int)l.ld_k : 0;
+    l.window = direct && !l.raw_any && c.D % 64 != 0 ? (int)l.ld_k : 0;
     l.ld_a = l.ld_k + (l.window ? 64 : 0);
     l.ld_acc = up(c.D, 8);
     if (l.f16) {
@@ -1453,7 +1536,7 @@ size_t xent_workspace(const XentCall& c, bool grads, bool least) {
     // Whether W can be read as it is its address and leading dimension say, call by call: room for both ways.  Packed rows of it take as much as W
     // itself where they are all there at once, so this way's room ends at kXePackedBytes (65536 x 4096, rows at odd places, 24 rows: loss 764
     // us with what the other way takes, 19 pieces, and 326 in one; with gradients 2305 and 636).
-    const bool as_is = direct || (!c.w_bf16 && !grads && c.n <= 64 && c.D % 4 == 0 && c.D >= 64);
+    const bool as_is = direct || (!c.w_bf16 && !grads && c.n <= 64 && raw_pays(c));
     for (int g = 0; g <= (grads ? 1 : 0); ++g)
         for (int f = g ? 0 : 1; f < 2; ++f) {
             if (as_is) {
@@ -1541,7 +1624,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     };
     XentProduct scores{};
     scores.y = l.f16 ? A16 : A; scores.ldy = l.f16 ? l.ld_k : l.ld_a; scores.y_plane = l.f16 ? a16_plane : a_plane; scores.y_rows = (int)l.n_padded;
-    scores.N = (int)n_some; scores.k_tiles = l.k_tiles;
+    scores.N = (int)n_some; scores.k_tiles = l.k_tiles; scores.x_cols = (int)c.D;
     scores.last_x = l.window ? (int)c.D - 64 : 64 * (l.k_tiles - 1);
     scores.last_y = l.window ? l.window : 64 * (l.k_tiles - 1);
     scores.pairs = l.f16 ? pair_list(l.w16_terms, l.a16_terms, l.score_most, &scores.pair_x, &scores.pair_y) : 1;
@@ -1604,8 +1687,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             scores_of(first, n, w);
             scores.partial = (float2*)(ws + l.partial) + tiles;
             if (l.raw) {
-                e = c.a_bf16 ? (n_some > 32 ? launch_raw_scores<2, 1>(scores, s) : launch_raw_scores<1, 1>(scores, s))
-                             : (n_some > 32 ? launch_raw_scores<2, 3>(scores, s) : launch_raw_scores<1, 3>(scores, s));
+                e = l.raw_any ? launch_raw_scores<true>(scores, c.a_bf16, (int)n_some, s) : launch_raw_scores<false>(scores, c.a_bf16, (int)n_some, s);
             } else {
                 e = l.f16 ? launch_product<false, false, true, kXeStats, float>(scores, l.scores.tile, s)
                           : launch_product<false, false, false, kXeStats, float>(scores, l.scores.tile, s);

@@ -111,3 +111,22 @@ def test_loss_of_more_scores_than_a_launch_takes():
     assert (loss[5::1000] == 0).all() and torch.isfinite(loss).all()
     want = _formula(W, a[rows], y[rows])
     _check(dict(loss=loss[rows], lse=lse[rows]), want, "f32", "f32", D, "rows")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,J,D,pad,offset", [(1, 3000, 1, 0, 0), (2, 129, 3, 1, 1), (64, 5000, 63, 0, 2), (1, 20000, 64, 1, 0), (33, 20001, 65, 0, 0), (64, 30000, 66, 2, 1),
+                                              (32, 40000, 127, 0, 3), (5, 40000, 130, 0, 0), (64, 20000, 193, 0, 0), (31, 20000, 254, 1, 1), (1, 24000, 259, 0, 0),
+                                              (64, 16001, 321, 4, 1), (7, 16000, 383, 0, 0), (33, 16000, 447, 0, 0), (1, 16000, 511, 2, 3), (64, 33000, 1025, 0, 0),
+                                              (20, 40000, 2047, 0, 1)])
+def test_loss_of_few_rows_with_fp32_words_at_any_place(n, J, D, pad, offset, dtype):
+    """W in fp32 with rows that neither start nor end at 16-byte places, one to thirty-two stages of 64 features; NaN between the rows."""
+    import paper_1511_08486_amd as sfb
+    W, a, y = _inputs(n, J, D, dtype, "f32", 90 + n, pad=pad, offset=offset, padded=0.2 if n > 2 else 0.0)
+    weight = torch.rand(n, generator=torch.Generator().manual_seed(1)).to(DEV)
+    want = _formula(W, a, y, weight, mean=True)
+    for least in (False, True):
+        _check(_loss(W, a, y, dtype, "f32", weight=weight, least=least), want, dtype, "f32", D, f"{n} {J} {D} least {least}")
+    head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype="f32", gradients=False)
+    head.loss(W, a, y, loss=torch.empty(n, device=DEV))
+    head.sync()
+    assert "raw" in _product(head)
