@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import test_xent_terms as terms
 from test_gpu_xent import DEV, PAIRS, TYPES, _check, _formula, _inputs, _run
 
 pytestmark = pytest.mark.gpu
@@ -130,3 +131,57 @@ def test_loss_of_few_rows_with_fp32_words_at_any_place(n, J, D, pad, offset, dty
     head.loss(W, a, y, loss=torch.empty(n, device=DEV))
     head.sync()
     assert "raw" in _product(head)
+
+
+@pytest.mark.parametrize("dtype,w_dtype", terms.PAIRS)
+@pytest.mark.parametrize("n,J,D", terms.CASES)
+def test_every_term_of_an_fp32_operand_is_in(n, J, D, dtype, w_dtype):
+    """Bounds that a product with a term less does not keep (tests/test_xent_terms.py shows that): losses, gradients alone and in one call."""
+    import paper_1511_08486_amd as sfb
+    cpu = terms.inputs(n, J, D, dtype, w_dtype, n)
+    W, a, y, weight = (x.to(DEV) for x in cpu)
+    back = lambda o: {k: v.cpu() for k, v in o.items()}  # noqa: E731
+    head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype=w_dtype)
+    head._ws.fill_(255)
+    o = dict(loss=torch.empty(n, device=DEV), lse=torch.empty(n, device=DEV))
+    head.loss(W, a, y, **o)
+    head.sync()
+    terms.check_loss(back(o), *cpu[:3])
+    grads = dict(dA=torch.empty_like(a), dW=torch.empty_like(W))
+    head.gradients(W, a, y, o["lse"], **grads, weight=weight)
+    head.sync()
+    terms.check_gradients(back(grads), *cpu, o["lse"].cpu())
+    both = dict(loss=torch.empty(n, device=DEV), lse=torch.empty(n, device=DEV), dA=torch.empty_like(a), dW=torch.empty_like(W))
+    head.loss_and_gradients(W, a, y, **both, weight=weight)
+    head.sync()
+    both = back(both)
+    terms.check_loss(both, *cpu[:3])
+    terms.check_gradients(both, *cpu, both["lse"])
+
+
+@pytest.mark.parametrize("n,J,D,pad,padded", [(1, 9000, 2048, 0, 0.0), (7, 131, 128, 8, 0.4), (33, 9001, 1984, 64, 0.5), (64, 20000, 2048, 8, 1.0)])
+def test_loss_of_few_rows_where_they_lie_on_the_least_workspace(n, J, D, pad, padded):
+    import paper_1511_08486_amd as sfb
+    for rows in (n, n + 100):
+        W, a, y = _inputs(n, J, D, "bf16", "bf16", 41, pad=pad, padded=padded)
+        want = _formula(W, a, y, mean=True)
+        _check(_loss(W, a, y, "bf16", "bf16", rows=rows, least=True), want, "bf16", "bf16", D, f"{n} {J} {D} rows {rows}")
+        least = sfb.SoftmaxHead(J, D, rows).least_bytes
+        head = sfb.SoftmaxHead(J, D, rows, workspace_bytes=least)
+        assert head._ws.numel() == max(least, 256)
+        head._ws.fill_(255)
+        o = dict(loss=torch.empty(n, device=DEV), lse=torch.empty(n, device=DEV), total=torch.empty(1, device=DEV))
+        head.loss(W, a, y, **o, mean=True)
+        head._ws.fill_(255)
+        grads = dict(dA=torch.empty_like(a), dW=torch.empty_like(W))
+        head.gradients(W, a, y, o["lse"], **grads, mean=True)
+        head.sync()
+        _check(dict(o, **grads), want, "bf16", "bf16", D, f"{n} {J} {D} rows {rows}")
+
+
+@pytest.mark.parametrize("dtype,w_dtype", PAIRS)
+def test_rows_that_a_launch_of_their_own_lists(dtype, w_dtype):
+    """More than 1024 rows, in every pair of types, some without a label, with room to spare and with the least."""
+    for ws in (None, 1e-9):
+        _run(1030, 700, 136, dtype, w_dtype, seed=61, padded=0.3, weighted=True, rows=1100, ws=ws)
+        _run(2100, 300, 72, dtype, w_dtype, seed=62, padded=0.97, mean=False, scale=0.5, ws=ws, two=True)
