@@ -303,7 +303,8 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
  *     u_ij = f w_i (exp(z_ij - lse_i) - [j = y(i)])       dA = U W  [n][D]       dW = U^T A  [J][D]
  * with w_i = weight[i] or 1, and f = scale, or scale divided by the number of rows that take part (mean != 0).  A row whose label lies outside
  * [0, J) takes no part: its loss, lse and row of dA are 0, and its features do not matter (any values, NaN too, in memory of the call's).  Rows n and
- * beyond of no output are touched; n = 0 is an empty batch (total = 0, dW = 0).
+ * beyond of no output are touched; n = 0 is an empty batch (total = 0, dW = 0).  A feature that is not finite, in a row that takes part, stays in that
+ * row's loss, lse and dA (none of them finite), and is in all of dW; a word of W with a NaN is in every loss.
  *   W, a        each in its own dtype: bf16 products are taken as they are, fp32 operands as two fp16 terms of every row divided by its own
  *               power of two (22 bits of a value above 2^-29 of its row's largest), for dW as three bf16 terms (exact); sums in fp32
  *   dA, dW      in the types of a and W, or NULL: not wanted.  With both in bf16 U is rounded to bf16 on the way, before f is applied (with

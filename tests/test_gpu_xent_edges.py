@@ -185,3 +185,36 @@ def test_rows_that_a_launch_of_their_own_lists(dtype, w_dtype):
     for ws in (None, 1e-9):
         _run(1030, 700, 136, dtype, w_dtype, seed=61, padded=0.3, weighted=True, rows=1100, ws=ws)
         _run(2100, 300, 72, dtype, w_dtype, seed=62, padded=0.97, mean=False, scale=0.5, ws=ws, two=True)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,J,D,dtype,w_dtype,pad", [(5, 900, 128, "bf16", "bf16", 0), (70, 900, 136, "bf16", "bf16", 0), (40, 700, 1600, "bf16", "bf16", 0), (70, 600, 136, "f32", "f32", 0),
+                                                     (40, 700, 1600, "f32", "f32", 0), (20, 24000, 192, "bf16", "f32", 0), (20, 24000, 192, "f32", "f32", 1), (20, 900, 72, "f32", "bf16", 0)])
+def test_a_feature_that_is_not_finite_stays_in_its_row(n, J, D, dtype, w_dtype, pad, bad):
+    """The row's own loss and gradient are not finite, and with it all of dW; the other rows' are what they are without it."""
+    import paper_1511_08486_amd as sfb
+    W, a, y = _inputs(n, J, D, dtype, w_dtype, 71, pad=pad)
+    want, others = _formula(W, a, y), torch.arange(n, device=DEV) != 3
+    a[3, D // 2] = bad
+    o = dict(loss=torch.empty(n, device=DEV), lse=torch.empty(n, device=DEV), dA=torch.empty((n, D), dtype=a.dtype, device=DEV), dW=torch.empty((J, D), dtype=W.dtype, device=DEV))
+    head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype=w_dtype)
+    for call in ("both", "loss"):
+        if call == "both":
+            head.loss_and_gradients(W, a, y, **o)
+        else:
+            o["loss"].zero_()
+            head.loss(W, a, y, loss=o["loss"], lse=o["lse"])
+        head.sync()
+        assert not torch.isfinite(o["loss"][3]) and not torch.isfinite(o["lse"][3])
+        assert not torch.isfinite(o["dA"][3].float()).any() and not torch.isfinite(o["dW"].float()).any()
+        _check({k: o[k][others] for k in ("loss", "lse", "dA")}, {k: v[others] if v.shape[:1] == (n,) and k != "total" else v for k, v in want.items()},
+               dtype, w_dtype, D, f"{call}: the other rows")
+
+
+@pytest.mark.parametrize("n,J,D,dtype,w_dtype,pad", [(5, 900, 128, "bf16", "bf16", 0), (70, 900, 136, "bf16", "bf16", 0), (70, 600, 136, "f32", "f32", 0), (40, 700, 1600, "f32", "f32", 0),
+                                                     (20, 24000, 192, "bf16", "f32", 0), (20, 24000, 192, "f32", "f32", 1)])
+def test_a_word_that_is_nan_is_in_every_loss(n, J, D, dtype, w_dtype, pad):
+    W, a, y = _inputs(n, J, D, dtype, w_dtype, 72, pad=pad)
+    W[J // 2, D - 1] = float("nan")
+    o = _loss(W, a, y, dtype, w_dtype)
+    assert torch.isnan(o["loss"]).all() and torch.isnan(o["lse"]).all() and torch.isnan(o["total"]).all()
