@@ -1375,8 +1375,10 @@ struct Layout {
 // Whether fp32 words read as they are give the loss of few rows sooner than their terms do.  Reading them takes a stage's latency after another, its
 // workgroups have all of D; terms cost W two more passes at 5.4 TB/s and 4 us, and their product is cut into slices of D.  One row of
 // bf16, as they are and as terms: 1000 x 1024 27 us and 16, 1000 x 8192 146 and 41, 4000 x 2048 44 and 34, 8000 x 4096 78 and 78, 16000 x 2048 45
-// and 72, 16000 x 8192 164 and 371; 64 rows of fp32: 1000 x 4096 120 and 33, 16000 x 4096 134 and 250.  The choice loses 16 % at most there.
+// and 72, 16000 x 8192 164 and 371; 64 rows of fp32: 1000 x 4096 120 and 33, 16000 x 4096 134 and 250, 10000 x 21504 670 and 1104.  The choice
+// loses 16 % at most there.
 static bool raw_pays(const XentCall& c) {
+    if (c.J > 63 * 128) return true;                                     // 64 tiles and more are not sliced
     const double stage_us = c.a_bf16 ? (c.n > 32 ? 1.20 : 1.06) : (c.n > 32 ? 1.63 : 1.23);
     return stage_us * (double)((c.D + 63) / 64) <= 4.0 + 2.2e-6 * (double)c.J * (double)c.D;
 }

@@ -46,7 +46,7 @@ def _product(head):
 def test_few_fp32_words_of_long_rows_are_cut_into_slices_of_features(n, dtype):
     """1000 words are eight workgroups where W is read as it is; more words of shorter rows fill the card that way."""
     import paper_1511_08486_amd as sfb
-    for J, D, as_it_is in ((1000, 8192, False), (24000, 512, True)):
+    for J, D, as_it_is in ((1000, 8192, False), (24000, 512, True), (8100, 12000, True)):
         W, a, y = _inputs(n, J, D, dtype, "f32", 80)
         head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype="f32", gradients=False)
         loss = torch.empty(n, device=DEV)
