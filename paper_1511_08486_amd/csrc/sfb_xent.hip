@@ -736,7 +736,143 @@ __global__ __launch_bounds__(256, ANY && TERMS == 1 ? 2 : 1) void xent_raw_score
     xe_wait_barrier();
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[0][j] += sum[j] + small[j];
+    if (a.out) {                                                         // rows are padded to whole tiles
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float* const z = reinterpret_cast<float*>(a.out) + (int64_t)(32 * j + l32) * a.ldo + m0 + wave * 32 + 4 * half;
+            if (32 * j + l32 < count)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4*>(z + 8 * q) = f32x4{acc[0][j][4 * q], acc[0][j][4 * q + 1], acc[0][j][4 * q + 2], acc[0][j][4 * q + 3]};
+        }
+        return;
+    }
     xe_stats_end<4, 1, NT, NT * 32>(a, acc, m0, 0, wave, 0, lane, count);
+}
+
+// dA of up to 64 rows with W in fp32 as it is, so that W's terms are never written: out[n][d] += sum_j U[n][j] W[j][d], U in its bf16 terms, W split into
+// terms in registers.  A wavefront has 128 d and all rows; a lane loads four d of a word at once, at any 4-byte place, and they belong to four
+// tiles of the matrix cores: tile c has d0 + 4 r + c for r = 0 .. 31, so that a lane also stores four d at once.  A row's last lanes load its last four
+// d again, and store what is their own.  Words go through registers, 32 ahead, U through LDS, 64 words a stage.  Blocks of 32 words are added up by
+// themselves.  MOST: pairs of terms whose numbers add up to so much at most.  65536 x 4096, 24 rows: 186 us, 5.8 TB/s; 64 of fp32 260.  (From terms
+// written before, 91 and 277, but writing them takes 400.)
+constexpr int kXeRawFeatures = 512;                                      // of a workgroup
+template <int NT, int MOST>
+__global__ __launch_bounds__(256, 1) void xent_raw_features_kernel(const XentProduct a) {
+    constexpr int TERMS = MOST + 1, Y_BYTES = NT * 32 * 128, STAGE = TERMS * Y_BYTES;
+    extern __shared__ __attribute__((aligned(16))) unsigned char xe_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5, count = *a.count;
+    if (count == 0) return;
+    const int split = blockIdx.x / a.m_tiles, d0 = (blockIdx.x % a.m_tiles) * kXeRawFeatures + wave * 128;
+    const int k_begin = min(split * a.per_split, a.k_tiles), k_end = min(k_begin + a.per_split, a.k_tiles);
+    const float* const W = reinterpret_cast<const float*>(a.x) + min(d0 + 4 * l32, a.M - 4);
+    uint32_t y_off[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+        y_off[i] = (uint32_t)((i * 4 + wave) * 8 + (lane >> 3)) * (uint32_t)a.ldy * 2u + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7) ^ (wave & 1)) * 16);
+    const uint32_t lds0 = xe_lds_address(xe_lds);
+    auto request_y = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+                xe_dma(a.y + t * a.y_plane + (int64_t)s * kXeK, y_off[i], lds0 + (s & 1) * STAGE + t * Y_BYTES + (i * 4 + wave) * 1024);
+    };
+    f32x16 acc[4][NT];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[c][j][e] = 0.f;
+    f32x4 first[16], second[16];                                         // the halves of a stage, on their way
+    auto load = [&](int s, int h, f32x4 (&w)[16]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int j = min(s * kXeK + 32 * h + 16 * (i >> 3) + 8 * half + (i & 7), a.x_rows - 1);   // (U is 0 from there on)
+            w[i] = *reinterpret_cast<const sp_f32x4u*>(W + (int64_t)j * a.ldx);
+        }
+    };
+    auto multiply = [&](int s, int h, const f32x4 (&w)[16]) __attribute__((always_inline)) {
+        const unsigned char* const now = xe_lds + (s & 1) * STAGE;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            sp_u32x4 x[2][TERMS];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    float v[4] = {w[8 * i + 4 * q][c], w[8 * i + 4 * q + 1][c], w[8 * i + 4 * q + 2][c], w[8 * i + 4 * q + 3][c]};
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) {
+                        const uint2 b = xe_bf4(v);
+                        x[i][t][2 * q] = b.x;
+                        x[i][t][2 * q + 1] = b.y;
+                    }
+                }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                sp_u32x4 y[2][TERMS];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t)
+                        y[i][t] = *reinterpret_cast<const sp_u32x4*>(now + t * Y_BYTES + (j * 32 + l32) * 128 +
+                                                                     (((4 * h + 2 * i + half) ^ (l32 & 7) ^ ((l32 >> 3) & 1)) << 4));
+                f32x16 block;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) block[e] = 0.f;
+#pragma unroll
+                for (int sum = MOST; sum >= 0; --sum)
+#pragma unroll
+                    for (int t = 0; t <= sum; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) block = split_mfma(x[i][t], y[i][sum - t], block);
+                acc[c][j] += block;
+            }
+        }
+    };
+    if (k_begin < k_end) {
+        request_y(k_begin);
+        __builtin_amdgcn_sched_barrier(0);
+        load(k_begin, 0, first);
+        for (int s = k_begin; s < k_end; ++s) {
+            __builtin_amdgcn_sched_barrier(0);
+            xe_stage_barrier<16>();                                      // U of this stage was requested before the sixteen loads on their way
+            if (s + 1 < k_end) request_y(s + 1);                         // into the buffer that everybody is through with
+            load(s, 1, second);
+            __builtin_amdgcn_sched_barrier(0);                           // (nothing that waits goes in front of the loads)
+            multiply(s, 0, first);
+            __builtin_amdgcn_sched_barrier(0);
+            load(s + 1, 0, first);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(s, 1, second);
+        }
+    }
+    float* const out = reinterpret_cast<float*>(a.out) + split * a.out_plane;
+    const float* const add = a.add ? a.add + split * a.out_plane : nullptr;
+    const float factor = *a.factor;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int n = 32 * j + l32;
+        if (n >= min(a.N, count)) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int d = d0 + 4 * (8 * (e / 4) + 4 * half + e % 4), base = min(d, a.M - 4);
+            if (d >= a.M) continue;
+            f32x4 v = f32x4{acc[0][j][e], acc[1][j][e], acc[2][j][e], acc[3][j][e]} * factor;
+            float* const o = out + (int64_t)n * a.ldo + base;
+            if (base == d) {                                             // (rows of the accumulators are whole multiples of 8)
+                if (add) v += *reinterpret_cast<const f32x4*>(add + (int64_t)n * a.ld_add + d);
+                *reinterpret_cast<f32x4*>(o) = v;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (base + c >= d) o[c] = v[c] + (add ? add[(int64_t)n * a.ld_add + base + c] : 0.f);
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -1263,6 +1399,15 @@ static hipError_t launch_raw_scores(const XentProduct& a, hipStream_t s) {
     SFB_LAUNCH((xent_raw_scores_kernel<NT, TERMS, ANY>), dim3((uint32_t)((a.M + kXeRawWords - 1) / kXeRawWords)), dim3(256), lds, s, a);
     return hipGetLastError();
 }
+template <int NT, int MOST>
+static hipError_t launch_raw_features(XentProduct a, hipStream_t s) {
+    constexpr size_t lds = 2 * (size_t)(MOST + 1) * NT * 32 * 128;
+    static_assert(lds <= 64 * 1024, "without being told to the runtime");
+    a.m_tiles = (a.M + kXeRawFeatures - 1) / kXeRawFeatures;
+    a.per_split = (a.k_tiles + a.splits - 1) / a.splits;
+    SFB_LAUNCH((xent_raw_features_kernel<NT, MOST>), dim3((uint32_t)(a.m_tiles * a.splits)), dim3(256), lds, s, a);
+    return hipGetLastError();
+}
 template <bool ANY>
 static hipError_t launch_raw_scores(const XentProduct& a, bool a_bf16, int rows, hipStream_t s) {
     if (a_bf16) return rows > 32 ? launch_raw_scores<2, 1, ANY>(a, s) : launch_raw_scores<1, 1, ANY>(a, s);
@@ -1377,10 +1522,18 @@ struct Layout {
 // bf16, as they are and as terms: 1000 x 1024 27 us and 16, 1000 x 8192 146 and 41, 4000 x 2048 44 and 34, 8000 x 4096 78 and 78, 16000 x 2048 45
 // and 72, 16000 x 8192 164 and 371; 64 rows of fp32: 1000 x 4096 120 and 33, 16000 x 4096 134 and 250, 10000 x 21504 670 and 1104.  The choice
 // loses 16 % at most there.
-static bool raw_pays(const XentCall& c) {
+// With gradients terms are written once for scores and dA, and the scores' product is sliced at any number of words: one row of bf16, as they are
+// and as terms: 500 x 512 34 and 45 (scores formed twice), 1000 x 4096 100 and 46, 8000 x 8192 297 and 289, 32000 x 512 85 and 95, 65536 x 4096 819 and 1129;
+// 64 rows of fp32: 4000 x 2048 114 and 73, 8000 x 8192 435 and 376, 32000 x 2048 287 and 382, 65536 x 4096 1033 and 1516.  It loses a twentieth.
+static bool raw_pays(const XentCall& c, bool grads) {
+    const double stage_us = c.a_bf16 ? (c.n > 32 ? 1.20 : 1.06) : (c.n > 32 ? 1.63 : 1.23), own_us = stage_us * (double)((c.D + 63) / 64);
+    if (grads) {
+        if (c.D < 64 || (size_t)64 * up(c.J, 256) * 4 > kXeScoreBytes) return false;
+        const double more_us = c.D * (c.a_bf16 ? 2 : 3) < 1500 ? 12.0 : -2.0;
+        return own_us <= more_us + (c.a_bf16 ? 1.9e-6 : 2.7e-6) * (double)c.J * (double)c.D;
+    }
     if (c.J > 63 * 128) return true;                                     // 64 tiles and more are not sliced
-    const double stage_us = c.a_bf16 ? (c.n > 32 ? 1.20 : 1.06) : (c.n > 32 ? 1.63 : 1.23);
-    return stage_us * (double)((c.D + 63) / 64) <= 4.0 + 2.2e-6 * (double)c.J * (double)c.D;
+    return own_us <= 4.0 + 2.2e-6 * (double)c.J * (double)c.D;
 }
 
 // Rows of W that LDS-DMA takes: pieces of 16 bytes, 32-bit offsets
@@ -1391,7 +1544,7 @@ static bool words_in_pieces(const XentCall& c) {
 // Rows of W that a product reads as they are: in bf16 with bf16 features, in pieces; in fp32 for the loss of few rows.
 static bool reads_w_directly(const XentCall& c, bool grads) {
     if (c.w_bf16) return c.a_bf16 && words_in_pieces(c);
-    return !grads && c.n <= 64 && raw_pays(c);
+    return c.n <= 64 && raw_pays(c, grads);
 }
 
 // piece: words of a piece, a multiple of 256
@@ -1421,18 +1574,23 @@ static Layout layout_of(const XentCall& c, bool direct, bool grads, bool kept, i
         l.a_terms = grads ? (c.a_bf16 ? 1 : l.dW_most + 1) : 0;
     } else {
         l.a_terms = l.raw && !c.a_bf16 ? 3 : 1;
-        l.u_terms = grads ? 1 : 0;
+        l.u_terms = !grads ? 0 : l.raw ? 3 : 1;
+        l.dW_most = l.raw ? 2 : 0;
     }
     const int score_pairs = l.f16 ? pair_count(l.w16_terms, l.a16_terms, 1) : 1;
     const int64_t row_tiles = (n + 63) / 64, word_tiles = (words + 63) / 64;
     l.ld_z = up(c.J, 256);
-    const int64_t planes = (int64_t)(kXeScoreBytes / ((size_t)l.n_padded * l.ld_z * 4)), slices = !kept || planes < 1 ? 1 : planes < 16 ? planes : 16;
+    const int64_t planes = (int64_t)(kXeScoreBytes / ((size_t)l.n_padded * l.ld_z * 4)), slices = !kept || l.raw || planes < 1 ? 1 : planes < 16 ? planes : 16;
     l.scores = tiling_for(words, n, (int64_t)l.k_tiles * score_pairs, slices, true, false,
                           kept ? kXeStore : grads ? kXeU : kXeStats, kept ? 4.0 : 2.0 * (l.u_terms + l.u16_terms));
     if (grads) {
         l.dA = tiling_for(c.D, n, word_tiles * (l.f16 ? pair_count(l.w16_terms, l.u16_terms, l.dA_most) : 1), 64, true, true, kXeStore, 4.0);
+        if (l.raw) {                                                     // a workgroup a compute unit
+            const int64_t tiles = (c.D + kXeRawFeatures - 1) / kXeRawFeatures;
+            l.dA.splits = tiles < 2 ? 128 : tiles < 256 ? (int)(256 / tiles) : 1;
+        }
         if (l.dA.splits > word_tiles) l.dA.splits = (int)word_tiles;
-        l.dW = tiling_for(c.D, words, row_tiles * (l.f16 ? pair_count(l.a_terms, l.u_terms, l.dW_most) : 1), 1, false, true, kXeStore, c.w_bf16 ? 2.0 : 4.0);
+        l.dW = tiling_for(c.D, words, row_tiles * pair_count(l.a_terms, l.u_terms, l.dW_most), 1, false, true, kXeStore, c.w_bf16 ? 2.0 : 4.0);
     }
     if (l.scores.splits > l.k_tiles) l.scores.splits = l.k_tiles;
     size_t at = 0;
@@ -1494,7 +1652,8 @@ static bool keeps_scores(const XentCall& c, bool direct, bool forward, bool grad
 // The layout that a call on c's sizes takes within `bytes`; .bytes > bytes: there is none
 static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads, size_t bytes) {
     const int64_t whole = up(c.J, 256) / 256;
-    for (int kept = !(direct && !c.w_bf16) && keeps_scores(c, direct, forward, grads); kept >= 0; --kept) {
+    const bool raw = direct && !c.w_bf16;                                // keeps its scores if gradients follow, and has no other way
+    for (int kept = raw ? grads : keeps_scores(c, direct, forward, grads); kept >= 0; --kept) {
         // a launch has fewer than 2^32 threads, 256 for 128 x 128 results: fewer than 2^38 scores a piece
         const int64_t launch_most = (((int64_t)1 << 37) / up(c.n > 0 ? c.n : 1, 256)) / 256;
         if (!grads && direct) {
@@ -1518,7 +1677,7 @@ static Layout plan_call(const XentCall& c, bool direct, bool forward, bool grads
         const int64_t pieces = (whole + lo - 1) / lo;                    // evened out
         Layout l = layout_of(c, direct, grads, kept != 0, (whole + pieces - 1) / pieces * 256);
         if (l.bytes > bytes) l = layout_of(c, direct, grads, kept != 0, lo * 256);
-        if (l.bytes <= bytes || !kept) return l;
+        if (l.bytes <= bytes || !kept || raw) return l;
     }
     return Layout{};                                                     // (not reached)
 }
@@ -1538,8 +1697,8 @@ size_t xent_workspace(const XentCall& c, bool grads, bool least) {
     // Whether W can be read as it is its address and leading dimension say, call by call: room for both ways.  Packed rows of it take as much as W
     // itself where they are all there at once, so this way's room ends at kXePackedBytes (65536 x 4096, rows at odd places, 24 rows: loss 764
     // us with what the other way takes, 19 pieces, and 326 in one; with gradients 2305 and 636).
-    const bool as_is = direct || (!c.w_bf16 && !grads && c.n <= 64 && raw_pays(c));
-    for (int g = 0; g <= (grads ? 1 : 0); ++g)
+    for (int g = 0; g <= (grads ? 1 : 0); ++g) {
+        const bool as_is = direct || (!c.w_bf16 && c.n <= 64 && raw_pays(c, g != 0));
         for (int f = g ? 0 : 1; f < 2; ++f) {
             if (as_is) {
                 const size_t b = plan_call(c, true, f != 0, g != 0, ~(size_t)0).bytes;
@@ -1548,12 +1707,14 @@ size_t xent_workspace(const XentCall& c, bool grads, bool least) {
             const size_t b = plan_call(c, false, f != 0, g != 0, as_is ? (m > kXePackedBytes ? m : kXePackedBytes) : ~(size_t)0).bytes;
             if (b > m) m = b;
         }
+    }
     return m;
 }
 
 hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t s) {
-    const bool direct = reads_w_directly(c, grads);
-    const Layout l = plan_call(c, direct, forward, grads, c.ws_bytes);
+    bool direct = reads_w_directly(c, grads);
+    Layout l = plan_call(c, direct, forward, grads, c.ws_bytes);
+    if (l.raw && l.bytes > c.ws_bytes) l = plan_call(c, direct = false, forward, grads, c.ws_bytes);
     if (l.bytes > c.ws_bytes) return hipErrorInvalidValue;
     char* const ws = (char*)c.ws;
     int* const rows = (int*)(ws + l.rows);
@@ -1674,7 +1835,9 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             XentProduct p = scores;
             p.splits = l.scores.splits;
             p.out = (float*)(ws + l.z) + first; p.ldo = l.ld_z; p.out_plane = l.n_padded * l.ld_z;
-            e = l.f16 ? launch_product<false, false, true, kXeStore, float>(p, l.scores.tile, s) : launch_product<false, false, false, kXeStore, float>(p, l.scores.tile, s);
+            if (l.raw) e = l.raw_any ? launch_raw_scores<true>(p, c.a_bf16, (int)n_some, s) : launch_raw_scores<false>(p, c.a_bf16, (int)n_some, s);
+            else if (l.f16) e = launch_product<false, false, true, kXeStore, float>(p, l.scores.tile, s);
+            else e = launch_product<false, false, false, kXeStore, float>(p, l.scores.tile, s);
             if (e != hipSuccess) return e;
         }
         e = rows_of((pieces - 1) * l.piece, !forward);
@@ -1712,7 +1875,8 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
     }
     // with gradients the first workgroup of their first product does it
     float* total_left = forward && !total_done && grads ? c.total : nullptr;
-    if (forward && c.total && !total_done && !grads)
+    if (l.raw && !c.dW) total_left = nullptr;
+    if (forward && c.total && !total_done && !total_left)
         hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)loss, (const float*)g, (const int*)count, (const float*)factor, c.total);
     e = hipGetLastError();
     if (e != hipSuccess || !grads) return e;
@@ -1733,7 +1897,21 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             e = l.f16 ? launch_product<false, false, true, kXeU, float>(scores, l.scores.tile, s) : launch_product<false, false, false, kXeU, float>(scores, l.scores.tile, s);
             if (e != hipSuccess) return e;
         }
-        if (c.dA) {
+        if (c.dA && l.raw) {
+            XentProduct p{};
+            p.x = w.p; p.ldx = w.ld; p.x_rows = w.rows;
+            p.y = U; p.ldy = l.piece; p.y_plane = u_plane;
+            p.M = (int)c.D; p.N = (int)n_some;
+            p.k_tiles = (int)((n + 63) / 64);
+            p.factor = factor;
+            p.splits = l.dA.splits;
+            p.count = count;
+            p.out = ws + l.acc; p.ldo = l.ld_acc; p.out_plane = acc_plane;
+            p.add = i < pieces - 1 ? (const float*)(ws + l.acc) : nullptr; p.ld_add = l.ld_acc;
+            if (c.a_bf16) e = n_some > 32 ? launch_raw_features<2, 1>(p, s) : launch_raw_features<1, 1>(p, s);
+            else e = n_some > 32 ? launch_raw_features<2, 2>(p, s) : launch_raw_features<1, 2>(p, s);
+            if (e != hipSuccess) return e;
+        } else if (c.dA) {
             XentProduct p{};
             p.x = w.p; p.ldx = w.ld; p.x_plane = w.plane; p.x_rows = w.rows; p.x_cols = direct ? (int)c.D : (int)l.ld_k;
             p.y = l.f16 ? U16 : U; p.ldy = l.piece; p.y_plane = u_plane; p.y_rows = (int)l.n_padded;
@@ -1764,7 +1942,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             p.y = U; p.ldy = l.piece; p.y_plane = u_plane; p.y_rows = (int)l.n_padded; p.y_cols = (int)l.piece;
             p.M = (int)c.D; p.N = (int)n;
             p.k_tiles = (int)((n_some + 63) / 64);
-            p.pairs = l.f16 ? pair_list(l.a_terms, l.u_terms, l.dW_most, &p.pair_x, &p.pair_y) : 1;
+            p.pairs = pair_list(l.a_terms, l.u_terms, l.dW_most, &p.pair_x, &p.pair_y);
             p.splits = 1;
             p.count = count; p.k_is_rows = true;
             p.factor = factor;
@@ -1781,7 +1959,7 @@ hipError_t launch_xent(const XentCall& c, bool forward, bool grads, hipStream_t 
             if (e != hipSuccess) return e;
         }
     }
-    if (c.dA && l.dA.splits > 1) {
+    if (c.dA && (l.dA.splits > 1 || l.raw)) {
         const uint32_t grid = (uint32_t)((n_some * ((c.D + 3) / 4) + 255) / 256);
         if (c.a_bf16)
             hipLaunchKernelGGL(xent_rows_out_kernel<bf16_t>, dim3(grid), dim3(256), 0, s, (const float*)(ws + l.acc), l.ld_acc, acc_plane, l.dA.splits,

@@ -218,3 +218,63 @@ def test_a_word_that_is_nan_is_in_every_loss(n, J, D, dtype, w_dtype, pad):
     W[J // 2, D - 1] = float("nan")
     o = _loss(W, a, y, dtype, w_dtype)
     assert torch.isnan(o["loss"]).all() and torch.isnan(o["lse"]).all() and torch.isnan(o["total"]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,J,D,pad,offset", [(1, 500, 64, 0, 0), (64, 130, 65, 0, 1), (33, 1000, 67, 1, 0), (20, 3000, 130, 0, 2), (64, 257, 447, 0, 0), (5, 12000, 513, 2, 3),
+                                              (32, 12000, 515, 0, 0), (40, 12001, 1022, 1, 1), (1, 20000, 1025, 0, 0), (64, 12000, 1540, 0, 0), (24, 12000, 2051, 3, 0)])
+def test_gradients_of_few_rows_with_fp32_words_at_any_place(n, J, D, pad, offset, dtype):
+    import paper_1511_08486_amd as sfb
+    _run(n, J, D, dtype, "f32", seed=100 + n, pad=pad, offset=offset, padded=0.2 if n > 2 else 0.0, weighted=True, scale=1.5)
+    _run(n, J, D, dtype, "f32", seed=100 + n, pad=pad, offset=offset, mean=False, out_pad=3, out_offset=1, two=True)
+    W, a, y = _inputs(n, J, D, dtype, "f32", 1, pad=pad, offset=offset)
+    head = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype="f32")
+    head.loss_and_gradients(W, a, y, dA=torch.empty_like(a))
+    head.sync()
+    assert "raw" in _product(head)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,J,D", [(40, 20000, 520), (7, 15003, 1100)])
+def test_gradients_of_few_rows_with_fp32_words_in_pieces(n, J, D, dtype):
+    for ws in (1e-9, 0.1, 0.2, 0.3, 0.45, 0.6, 0.8):
+        _run(n, J, D, dtype, "f32", seed=120, ws=ws, padded=0.1, two=ws == 0.45)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_gradient_of_few_rows_with_fp32_words_and_the_total(dtype):
+    import paper_1511_08486_amd as sfb
+    n, J, D = 30, 4000, 260
+    W, a, y = _inputs(n, J, D, dtype, "f32", 121, padded=0.2)
+    head, want = sfb.SoftmaxHead(J, D, n, dtype=dtype, w_dtype="f32"), _formula(W, a, y, mean=True)
+    for k, like in (("dA", a), ("dW", W)):
+        o = {"total": torch.zeros(1, device=DEV), k: torch.empty(like.shape, dtype=like.dtype, device=DEV)}
+        head._ws.fill_(255)
+        head.loss_and_gradients(W, a, y, **o, mean=True)
+        head.sync()
+        _check(o, want, dtype, "f32", D, k)
+
+
+def test_few_rows_with_fp32_words_recorded_in_a_graph():
+    import paper_1511_08486_amd as sfb
+    n, J, D = 24, 6000, 322
+    side = torch.cuda.Stream(device=DEV)
+    W, a, y = _inputs(n, J, D, "f32", "f32", 122)
+    outs = lambda: dict(loss=torch.zeros(n, device=DEV), lse=torch.zeros(n, device=DEV), dA=torch.zeros(n, D, device=DEV), dW=torch.zeros(J, D, device=DEV),  # noqa: E731
+                        total=torch.zeros(1, device=DEV))
+    eager, taken = (sfb.SoftmaxHead(J, D, n, dtype="f32", w_dtype="f32", stream=side.cuda_stream) for _ in range(2))
+    e, t = outs(), outs()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        taken.loss_and_gradients(W, a, y, **t, mean=True)
+    for k in range(4):
+        y.copy_(torch.where(torch.arange(n, device=DEV) % 3 == k % 3, -1, (y.clamp(min=0) * 7 + k) % J))
+        a.mul_(-1.0)
+        torch.cuda.synchronize()
+        eager.loss_and_gradients(W, a, y, **e, mean=True)
+        eager.sync()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(e[x], t[x]) for x in e), k
+        _check(t, _formula(W, a, y, mean=True), "f32", "f32", D, f"replay {k}")
