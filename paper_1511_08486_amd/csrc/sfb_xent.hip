@@ -22,7 +22,7 @@
 //
 // Bound by: many rows, the matrix cores at the clock that they hold (131072 words, 4096 rows and features, bf16: scores 1.20 PFLOP/s, with U
 // 1.10, dA 1.30, dW 1.18, the clock at 1.63 GHz, 64 to 75 % of its cycles in matrix instructions, LDS a fifth, no bank conflicts); few rows, W's
-// way from memory (65536 x 4096 in bf16, 24 rows: 112 us, 4.8 TB/s).
+// way from memory (65536 x 4096 in bf16, 24 rows: 109 us, 4.9 TB/s).
 #include "sfb_kernels.h"
 #include "sfb_split.h"
 
@@ -569,8 +569,8 @@ __global__ __launch_bounds__(WGM * WGN * 64, OCC) void xent_product_kernel(const
 // Scores of up to 64 rows with W in fp32 as it is: W goes to LDS raw and is split into three bf16 terms on its way to the matrix cores
 // (exact; six products with fp32 features, three with bf16 ones), so that it crosses memory once.  By the general way its terms are
 // written and read again.  128 words a workgroup, a stage of 64 k with all of the features' terms; two
-// stages, so that two workgroups fit a compute unit (65536 x 4096, one row of bf16: 235 us, 4.6 TB/s; one workgroup with three or four stages
-// 289; its terms packed first 728), three where only one fits anyway (fp32 features: 290; packed 917).  The leading products and the others have sums of their own, the former in blocks of 256 k.
+// stages, so that two workgroups fit a compute unit (65536 x 4096, one row of bf16: 190 us, 5.7 TB/s; its terms packed first 607), three where only
+// one fits anyway (fp32 features: 200; packed 700).  The leading products and the others have sums of their own, the former in blocks of 256 k.
 // LDS rows of W: 256 bytes, 16-byte piece p of row r at p ^ (r & 15).
 // ANY: rows of W at any 4-byte place and of any length.  They come through registers, two stages ahead, since LDS-DMA wants whole pieces at
 // 16-byte places; what lies behind a row is not read (65536 x 4096, rows 4097 apart: one row of bf16 199 us, 64 of fp32 289; their terms packed
@@ -593,11 +593,11 @@ __global__ __launch_bounds__(256, ANY && TERMS == 1 ? 2 : 1) void xent_raw_score
         y_off[i] = (uint32_t)((i * 4 + wave) * 8 + (lane >> 3)) * (uint32_t)a.ldy * 2u + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7) ^ (wave & 1)) * 16);
     const uint32_t lds0 = xe_lds_address(xe_lds);
     const int stages = a.k_tiles;
-    auto request_y = [&](int s) __attribute__((always_inline)) {
+    auto request_y = [&](int s, int k) __attribute__((always_inline)) {
         const uint32_t to = lds0 + (s % ST) * STAGE + X_BYTES;
 #pragma unroll
         for (int t = 0; t < TERMS; ++t) {
-            const bf16_t* const y = a.y + t * a.y_plane + (s == stages - 1 ? a.last_y : s * kXeK);
+            const bf16_t* const y = a.y + t * a.y_plane + (k == stages - 1 ? a.last_y : k * kXeK);
 #pragma unroll
             for (int i = 0; i < NT; ++i) xe_dma(y, y_off[i], to + t * Y_BYTES + (i * 4 + wave) * 1024);
         }
@@ -673,12 +673,12 @@ __global__ __launch_bounds__(256, ANY && TERMS == 1 ? 2 : 1) void xent_raw_score
         auto step = [&](int s, f32x4 (&w)[8]) __attribute__((always_inline)) {
             put(s, w);
             xe_stage_barrier<8>();
-            request_y(s + 1);
+            request_y(s + 1, s + 1);
             load(s + 2, w);
             asm volatile("" ::: "memory");                               // (the loads stay in front)
             multiply(s);
         };
-        request_y(0);
+        request_y(0, 0);
         int s = 0;
         if (full > 3) {                                                  // (no branch among the loads: waits are counted)
             load(0, even);
@@ -696,7 +696,7 @@ __global__ __launch_bounds__(256, ANY && TERMS == 1 ? 2 : 1) void xent_raw_score
         for (; s < full; ++s) {                                          // the last three at most
             put(s, even);
             xe_wait_barrier();
-            request_y(s + 1);
+            request_y(s + 1, s + 1);
             multiply(s);
 #pragma unroll
             for (int i = 0; i < 8; ++i) even[i] = odd[i];
@@ -718,12 +718,16 @@ __global__ __launch_bounds__(256, ANY && TERMS == 1 ? 2 : 1) void xent_raw_score
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             x_off[i] = (uint32_t)(min(m0 + i * 16 + in16, a.x_rows - 1) - m0) * (uint32_t)a.ldx * 4u + (uint32_t)(((lane & 15) ^ in16) * 16);
+        // Every workgroup begins a stage on from its neighbour and goes round: rows 2^14 bytes apart are on the same few memory channels where all
+        // workgroups read the same columns (65536 x 4096, one row of bf16 242 -> 190 us, of fp32 301 -> 200; 32768 x 4096 163 -> 110)
+        const int turn = (int)(blockIdx.x % (unsigned)stages);
         auto request = [&](int s) {
+            const int k = s + turn < stages ? s + turn : s + turn - stages;
             const uint32_t to = lds0 + (s % ST) * STAGE;
-            const float* const x = W + (s == stages - 1 ? a.last_x : s * kXeK);
+            const float* const x = W + (k == stages - 1 ? a.last_x : k * kXeK);
 #pragma unroll
             for (int i = 0; i < 8; ++i) xe_dma(x, x_off[i], to + (i * 4 + wave) * 1024);
-            request_y(s);
+            request_y(s, k);
         };
         for (int s = 0; s < min(ST - 1, stages); ++s) request(s);
         for (int s = 0; s < stages; ++s) {
