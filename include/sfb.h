@@ -306,10 +306,11 @@ SFB_API sfb_status sfb_step_prox(sfb_ctx *ctx, float *W, int64_t ldw, const sfb_
  * beyond of no output are touched; n = 0 is an empty batch (total = 0, dW = 0).  A feature that is not finite, in a row that takes part, stays in that
  * row's loss, lse and dA (none of them finite), and is in all of dW; a word of W with a NaN is in every loss.
  *   W, a        each in its own dtype: bf16 products are taken as they are, fp32 operands as two fp16 terms of every row divided by its own
- *               power of two (22 bits of a value above 2^-29 of its row's largest), for dW as three bf16 terms (exact); sums in fp32
+ *               power of two (22 bits of a value above 2^-29 of its row's largest), for dW, and where fp32 words meet up to 64 rows, as three
+ *               bf16 terms (exact); sums in fp32
  *   dA, dW      in the types of a and W, or NULL: not wanted.  With both in bf16 U is rounded to bf16 on the way, before f is applied (with
- *               the results' own rounding 1.2 times the error of that alone, 1.5 with weights of any size); otherwise it is kept in
- *               more terms
+ *               the results' own rounding 1.2 times the error of that alone, 1.5 with weights of any size).  dA in bf16 beside W in fp32 takes 11
+ *               bits of U and of W (16, up to 64 rows: less than its own rounding either way); otherwise U is kept in as many terms as W or a
  *   loss, lse, total, weight   DEVICE fp32, NULL: not wanted (lse is needed by sfb_xent_gradients, which reads what sfb_xent_loss left)
  *   ws          DEVICE, 256-byte aligned; it belongs to the call until that has run: calls that may overlap in time, replays of captured
  *               ones included, need one each.  sfb_xent_workspace_bytes: the least a call on up to P*B rows can take, and as much as
@@ -394,7 +395,8 @@ SFB_API sfb_status sfb_adamw_unpack(sfb_ctx *ctx, const sfb_adamw_tensor *tensor
 /*
  * The norm of many gradients taken as one vector, and the factor that clips them, both left on the device:
  *     out[0] = norm = sqrt(sum g^2)      out[1] = min(1, max_norm / norm), NaN if the norm is not finite
- * out: DEVICE [2] fp32.  The sum is taken in 64 bits in a fixed order.  ws: DEVICE, 8-byte aligned, at least sfb_grad_norm_bytes; it
+ * out: DEVICE [2] fp32.  The sum is taken in 64 bits in a fixed order, and so is the factor: a norm beyond fp32's range leaves infinity in
+ * out[0] and is clipped all the same.  ws: DEVICE, 8-byte aligned, at least sfb_grad_norm_bytes; it
  * belongs to the call until that has run (calls that may overlap in time need one each).
  * SFB_EINVAL: a null pointer, count < 0, max_norm not positive (infinity: no clipping); SFB_ESHAPE: n < 0 or beyond 2^40;
  * SFB_EDTYPE; SFB_EWORKSPACE.

@@ -18,6 +18,7 @@
 //                  are in U, and U's rows are divided by what their weight bounds them by.  A bf16 dA takes one term of each (2^-12).
 //   dW             three bf16 terms (exact) and six products (three with bf16 features): along its contraction, the rows, the factors of a
 //                  rare word may all be below 2^-40 of a label's, and must not be rounded by that.
+//   fp32 W, up to 64 rows   three bf16 terms of W, split where they are used, in scores and dA too (a bf16 dA: two)
 // Small problems keep their scores (256 MB at most, their slices of D included) where forming them again would take longer than reading them.
 //
 // Bound by: many rows, the matrix cores at the clock that they hold (131072 words, 4096 rows and features, bf16: scores 1.20 PFLOP/s, with U

@@ -17,7 +17,9 @@ class SoftmaxHead(_Stream):
     Owns an sfb_ctx and a workspace (workspace_bytes: as many, at least what the calls need; default: as many as speed them up).
     Rows whose label is outside [0, J) take no part.  Gradients come in the types of the features and of W; give one or both.
     `gradients` reads the lse that `loss` left; `loss_and_gradients` is both in one call.  Calls that may overlap in time, replays of
-    captured ones included, need a head each (it holds a workspace)."""
+    captured ones included, need a head each (it holds a workspace).
+    Calls run on `stream`, the one that was current at construction by default, whichever is current when they are made.  Work of other
+    streams on the same tensors is ordered by the caller, who also keeps them until the call has run."""
 
     def __init__(self, J, D, rows, dtype="bf16", w_dtype="bf16", workspace_bytes=None, gradients=True, stream=None, device="cuda:0"):
         self._a, self._w = _DTYPES[dtype], _DTYPES[w_dtype]

@@ -76,7 +76,8 @@ class GradNorm(_Stream):
     """The norm of `grads` (fp32 or bf16, all of one type) as one vector, and the factor that clips it:
     out[0] = norm, out[1] = min(1, max_norm / norm), NaN if the norm is not finite.  Both stay on the device; hand out[1:] to
     AdamW.step as grad_scale.  The gradients' memory is that of the construction; `grads` are kept alive with the object.  Calls that may
-    overlap in time, replays of captured ones included, need an object each (it holds a workspace)."""
+    overlap in time, replays of captured ones included, need an object each (it holds a workspace).  Calls run on `stream`, the one
+    that was current at construction by default; work of other streams on the same tensors is ordered by the caller."""
 
     def __init__(self, grads, stream=None, device="cuda:0"):
         super().__init__(stream, device)
@@ -98,7 +99,9 @@ class AdamW(_Stream):
     """AdamW over lists of tensors: params fp32, grads fp32 or bf16, first and second moments fp32 or, with m_scales and v_scales
     (uint8, one for every 128 elements), uint8 codes; copies: bf16 tensors that receive the rounded parameters, or None.
     `step` is a device int32 that holds the steps taken (0 at first) and goes on counting in a replayed graph.  8-bit moments start
-    as zeros.  All tensors are kept alive with the object and keep their memory; step(grads=...) takes others from then on."""
+    as zeros.  All tensors are kept alive with the object and keep their memory; step(grads=...) takes others from then on.
+    Steps run on `stream`, the one that was current at construction by default.  Work of other streams on the same tensors is ordered
+    by the caller, who keeps replaced gradients, and an object that is dropped, until the stream is through with them."""
 
     def __init__(self, params, grads, m, v, step, m_scales=None, v_scales=None, copies=None, stream=None, device="cuda:0"):
         super().__init__(stream, device)

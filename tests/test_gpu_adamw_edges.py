@@ -55,3 +55,13 @@ def test_8_bit_moments_of_elements_beyond_32_bits():
     # of elements that round up with a probability p, two draws differ with 2 p (1 - p): a third on average where p is anything
     moved = float((front[1] != behind[1]).double().mean())
     assert 0.2 < moved < 0.45, moved
+
+
+def test_norm_beyond_fp32_is_clipped_all_the_same():
+    import paper_1511_08486_amd as sfb
+    out = torch.zeros(2, device=DEV)
+    norm = sfb.GradNorm([torch.full((4,), 3e38, device=DEV)])
+    norm(1e3, out)
+    norm.sync()
+    assert float(out[0]) == float("inf")
+    assert abs(float(out[1]) / (1e3 / 6e38) - 1.0) <= 2.0 ** -22         # 3e38 and the factor as fp32 numbers
